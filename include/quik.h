@@ -76,6 +76,11 @@ typedef enum {
     QUIK_ELAUNCH = -6       /* the HIP runtime refused a launch                     */
 } quik_status;
 
+/* Types of activations and of router logits (w4g layers and layers of experts; every other entry point takes fp16). */
+typedef enum { QUIK_F16 = 0, QUIK_BF16 = 1, QUIK_F32 = 2 } quik_type;
+/* How a router turns logits into scores. */
+typedef enum { QUIK_SOFTMAX = 0, QUIK_SIGMOID = 1 } quik_score;
+
 /* Library version (monotonic integer). */
 int quik_version(void);
 
@@ -467,6 +472,76 @@ int quik_linear_sp24(const void *x, int T, int K, int ldx, const int32_t *outlie
                      const void *w24, const void *w_scale, const float *w_reduced,
                      const void *w_out, int ldwo, const void *bias, int N,
                      void *y, int ldy, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Layers with 4-bit weights in groups ("w4g"): a scale, and where there are any an integer zero point, for every `group`
+ * consecutive input columns of an output channel, under activations left at 16 bits (fp16 or bf16).  The form for
+ * decoding, where the weights are all the traffic and quantizing the activations saves nothing.
+ *
+ *   W[n, k] = w_scale[n, k / group] * (w_q[n, k] - w_zero[n, k / group])
+ *   a[t, n] = sum_k x[t, k] * W[n, k] (+ bias[n])
+ *   y[t, n] = a[t, n]                                          (glu = 0; y has N columns)
+ *   y[t, f] = a[t, f] * sigmoid(a[t, f]) * a[t, N / 2 + f]     (glu = 1; N even, y has N / 2 columns: the first half of the
+ *                                                              channels are gates, the second half values)
+ * Sums are fp32 and y is rounded once.  Up to 64 rows (experts: that few to an expert) the scale is applied to fp32 sums of
+ * exact products; above that the weights are first rounded to the type of x, one rounding per weight.
+ * A row of x with an infinity or a NaN gives a row of y without meaning; other rows are not affected.
+ *
+ *  quik_weight_pack_w4g   once per layer: codes, scales and zero points -> w4 (quik_w4g_bytes(...) bytes, 16-byte aligned).
+ *    w_q       packed signed 4-bit codes [N, ldw bytes] in the weight nibble order of this header, ldw >= K / 2
+ *    w_scale   fp16 [N, G], G = ceil(K / group)
+ *    w_zero    int8 [N, G], or NULL for none
+ *    group     32, 64 or a multiple of 128; 0: one group for the whole row (G = 1).  The last group of a row may be shorter
+ *    experts   1 for a layer; E for a layer of experts, whose w_q, w_scale and w_zero are [E, ...] without gaps
+ *  quik_linear_w4g        the layer.  x [T, ldx], bias [N] or NULL, y [T, ldy] of `type`; group, has_zero, glu, N and K are
+ *                         those that w4 was packed with.  One kernel launch, no workspace.
+ *
+ * Limits of these layers: T >= 1; K a multiple of 8, at most 32768; N at most 2^20; x and w4 16-byte aligned, ldx a
+ * multiple of 8; ldy >= the columns of y, y otherwise unconstrained; w_q 16-byte aligned, ldw a multiple of 16.  y does not
+ * overlap an input.
+ */
+size_t quik_w4g_bytes(int N, int K, int group, int has_zero, int glu, int experts);
+int quik_weight_pack_w4g(const void *w_q, int ldw, const void *w_scale, const void *w_zero, int N, int K, int group, int glu,
+                         int experts, void *w4, void *stream);
+int quik_linear_w4g(int type, const void *x, int T, int K, int ldx, const void *w4, int group, int has_zero, int glu,
+                    const void *bias, int N, void *y, int ldy, void *stream);
+
+/*
+ * Layers of experts: each token goes to top_k of `experts` w4g layers, which a router chooses.
+ *
+ *  quik_moe_route         the router.  For every token, out of its logits l [T, ldl] (`type`: fp16, bf16 or fp32):
+ *      score[e]  = softmax(l)[e] or sigmoid(l[e])   (`score`: QUIK_SOFTMAX, QUIK_SIGMOID)
+ *      choice[e] = score[e] + bias[e]               (bias fp32 [experts] or NULL: it decides who is chosen, nothing else)
+ *      the `groups` groups of experts / groups consecutive experts are ranked by the sum of their group_top largest
+ *        choices, and only the topk_groups first ones stay (groups = 1, topk_groups = 1: all stay)
+ *      ids[t, :]     = the top_k experts of the largest choices, largest first       int32 [T, top_k]
+ *      weights[t, :] = their scores, divided by their sum if `renormalize` (by nothing, and 0, if that is 0), times `scale`
+ *                                                                                    fp32 [T, top_k]
+ *    Ties go to the lowest index; choices are told apart as float64 tells them.  An expert whose logit is -infinity or NaN,
+ *    or whose choice is, takes no part (an infinite logit is the limit: the softmax is shared among those).  A slot that no
+ *    expert is left for gets id -1 and weight 0.
+ *    Limits: experts <= 1024, top_k <= 32, groups <= 64, group_top <= experts / groups, top_k <= topk_groups * experts / groups.
+ *
+ *  quik_moe_linear_w4g    the experts' products.  Row r = t * top_k + j is slot j of token t, of expert e = ids[r]:
+ *      a[r, n] = sum_k x[row, k] * W_e[n, k] (+ bias[e, n])   and glu as above, where `row` is t (x_per_slot = 0: x is
+ *                                                             [T, ldx]) or r (x_per_slot = 1: x is [T * top_k, ldx])
+ *      y[r, :] = a[r, :]                                      weights NULL: y is [T * top_k, ldy]
+ *      y[t, :] = sum_j weights[t, j] * a[t * top_k + j, :]    weights fp32 [T, top_k]: y is [T, ldy]; summed in fp32 in the
+ *                                                             order of the slots, rounded once
+ *    An id outside 0 .. experts - 1 (padding, an expert that another GPU holds) is no expert: its rows of y are zeros,
+ *    and it takes no part in a sum (its weight is not looked at).  The same expert twice in a token is two slots.
+ *      bias        [experts, N] or NULL
+ *      workspace   quik_moe_workspace_bytes(T, top_k, N, glu, experts, weights != NULL) bytes, 256-byte aligned; nothing
+ *                  has to be cleared, nothing is kept; calls that may overlap in time need one each
+ *    Limits: those of the w4g layers; T * top_k <= 2^24.
+ */
+int quik_moe_route(int type, const void *logits, int T, int experts, int ldl, const float *bias, int score, int groups,
+                   int topk_groups, int group_top, int top_k, int renormalize, float scale, int32_t *ids, float *weights,
+                   void *stream);
+size_t quik_moe_workspace_bytes(int T, int top_k, int N, int glu, int experts, int combine);
+int quik_moe_linear_w4g(int type, const void *x, int ldx, int x_per_slot, const int32_t *ids, const float *weights, int T,
+                        int top_k, int K, const void *w4, int group, int has_zero, int glu, const void *bias, int N,
+                        int experts, void *y, int ldy, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Measurement probes (not part of the layer): what the chip sustains, so that a kernel's rate can

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -119,6 +120,18 @@ def load() -> C.CDLL:
         lib.quik_linear_sp24.argtypes = [vp, i, i, i, vp, i, vp, vp, f, vp, i, vp, i, vp, i, vp, C.c_size_t, vp]
         lib.quik_linear_fp6.restype = i
         lib.quik_linear_fp6.argtypes = [vp, i, i, i, vp, i, vp, vp, f, vp, i, vp, i, vp, i, vp, C.c_size_t, vp]
+        lib.quik_w4g_bytes.restype = C.c_size_t
+        lib.quik_w4g_bytes.argtypes = [i, i, i, i, i, i]
+        lib.quik_weight_pack_w4g.restype = i
+        lib.quik_weight_pack_w4g.argtypes = [vp, i, vp, vp, i, i, i, i, i, vp, vp]
+        lib.quik_linear_w4g.restype = i
+        lib.quik_linear_w4g.argtypes = [i, vp, i, i, i, vp, i, i, i, vp, i, vp, i, vp]
+        lib.quik_moe_route.restype = i
+        lib.quik_moe_route.argtypes = [i, vp, i, i, i, vp, i, i, i, i, i, i, C.c_float, vp, vp, vp]
+        lib.quik_moe_workspace_bytes.restype = C.c_size_t
+        lib.quik_moe_workspace_bytes.argtypes = [i, i, i, i, i, i]
+        lib.quik_moe_linear_w4g.restype = i
+        lib.quik_moe_linear_w4g.argtypes = [i, vp, i, i, vp, vp, i, i, i, vp, i, i, i, vp, i, i, vp, i, vp, C.c_size_t, vp]
         lib.quik_debug_mfma_probe.restype = i
         lib.quik_debug_mfma_probe.argtypes = [i, i, vp, vp]
         lib.quik_debug_mix_probe.restype = i
@@ -895,3 +908,233 @@ def workspace_views(workspace, T: int, K: int, N: int, n_out: int, bits: int):
     zero = workspace[off[2]: off[2] + T * 4].view(torch.float32)
     x_out = workspace[off[3]: off[3] + T * n_out * 2].view(torch.float16).view(T, n_out)
     return xq, scale, zero, x_out
+
+
+# ---- layers with 4-bit weights in groups, and layers of experts
+
+_TYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+
+
+class WeightW4G(NamedTuple):
+    """What quik_weight_pack_w4g makes of a layer's weights, with the sizes that the products need beside them."""
+    data: torch.Tensor      # uint8 [quik_w4g_bytes]
+    N: int
+    K: int
+    group: int              # 0: the whole row
+    has_zero: bool
+    glu: bool
+    experts: int            # 0: one layer
+
+    @property
+    def width(self) -> int:
+        """Columns of the output."""
+        return self.N // 2 if self.glu else self.N
+
+
+def _matrix(t, dtypes, name, rows, cols, device):
+    """A [rows, cols] device matrix with contiguous rows -> its row stride in elements."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[1] != cols or (rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {cols}], got {list(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must be contiguous along its last dimension")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), (cols + 7) // 8 * 8)   # (one row has no stride)
+
+
+def _whole(t, dtype, name, shape, device):
+    """A contiguous device tensor of this shape, or None."""
+    if t is None:
+        return
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {list(shape)}, got {list(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _run_on(device, fn, name, args):
+    """fn(*args, stream) on the device's current stream, whatever the current device is."""
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream()), name)
+        return
+    with torch.cuda.device(device):
+        _check(fn(*args, _stream()), name)
+
+
+def _prepared_on(device, fn, name, args, keep):
+    """The same with everything looked up once: the stream is the device's current one now."""
+    with torch.cuda.device(device):
+        stream = _stream()
+    args = (*args, stream)
+
+    def call(_keep=keep):
+        if torch.cuda.current_device() == device.index:
+            rc = fn(*args)
+        else:
+            with torch.cuda.device(device):
+                rc = fn(*args)
+        if rc != 0:
+            raise QuikError(rc, name)
+    return call
+
+
+def quik_w4g_bytes(N: int, K: int, group: int, has_zero: bool = False, glu: bool = False, experts: int = 1) -> int:
+    return load().quik_w4g_bytes(N, K, group, int(has_zero), int(glu), experts)
+
+
+def quik_weight_pack_w4g(w_q, w_scale, K: int, group: int, w_zero=None, glu: bool = False) -> WeightW4G:
+    """Packed signed 4-bit codes uint8 [N, ldw] (ldw >= K / 2, a multiple of 16), scales fp16 [N, G] and zero points
+    int8 [N, G] or None, G = ceil(K / group), or 1 for group = 0 -> the layer's weights as the products read them.
+    With a leading dimension of experts on each: a layer of experts.  glu: the first half of the channels are gates, the
+    second half values, and the product returns silu(gate) * value."""
+    if not isinstance(w_q, torch.Tensor) or not w_q.is_cuda:
+        raise TypeError("w_q must be a device tensor")
+    if w_q.dtype != torch.uint8:
+        raise TypeError(f"w_q must be {torch.uint8}, got {w_q.dtype}")
+    if w_q.dim() not in (2, 3) or (w_q.numel() and not w_q.is_contiguous()):
+        raise ValueError("w_q must be contiguous, [N, ldw] or [experts, N, ldw]")
+    lead, N, ldw = tuple(w_q.shape[:-2]), w_q.shape[-2], w_q.shape[-1]
+    experts = lead[0] if lead else 1
+    need = quik_w4g_bytes(N, K, group, w_zero is not None, glu, experts)
+    if need == 0:
+        raise QuikError(load().quik_weight_pack_w4g(None, ldw, None, None, N, K, group, int(glu), experts, None, None),
+                        "quik_weight_pack_w4g")
+    G = 1 if group == 0 else -(-K // group)
+    if w_scale is None:
+        raise TypeError("w_scale must be a device tensor")
+    _whole(w_scale, torch.float16, "w_scale", (*lead, N, G), w_q.device)
+    _whole(w_zero, torch.int8, "w_zero", (*lead, N, G), w_q.device)
+    data = torch.empty(need, dtype=torch.uint8, device=w_q.device)
+    _run_on(w_q.device, load().quik_weight_pack_w4g, "quik_weight_pack_w4g",
+            (_ptr(w_q), ldw, _ptr(w_scale), _ptr(w_zero), N, K, group, int(glu), experts, _ptr(data)))
+    return WeightW4G(data, N, K, group, w_zero is not None, bool(glu), experts if lead else 0)
+
+
+def _w4g(w, x, experts: bool):
+    if not isinstance(w, WeightW4G):
+        raise TypeError("w must come from quik_weight_pack_w4g")
+    if bool(w.experts) != experts:
+        raise ValueError("w holds " + ("one layer, not experts" if experts else "experts: use quik_moe_linear_w4g"))
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError("x must be a device tensor")
+    _whole(w.data, torch.uint8, "w.data",
+           (quik_w4g_bytes(w.N, w.K, w.group, w.has_zero, w.glu, max(w.experts, 1)),), x.device)
+
+
+def _linear_w4g_args(x, w, bias, out):
+    _w4g(w, x, experts=False)
+    ldx = _matrix(x, (torch.float16, torch.bfloat16), "x", None, w.K, x.device)
+    T = x.shape[0]
+    _whole(bias, x.dtype, "bias", (w.N,), x.device)
+    y = torch.empty((T, w.width), dtype=x.dtype, device=x.device) if out is None else out
+    ldy = _matrix(y, (x.dtype,), "out", T, w.width, x.device)
+    return (_TYPES[x.dtype], _ptr(x), T, w.K, ldx, _ptr(w.data), w.group, int(w.has_zero), int(w.glu), _ptr(bias), w.N,
+            _ptr(y), ldy), y
+
+
+def quik_linear_w4g(x, w: WeightW4G, bias=None, out=None):
+    """x fp16 or bf16 [T, K] through a layer with 4-bit weights in groups -> y [T, w.width] of the same type."""
+    args, y = _linear_w4g_args(x, w, bias, out)
+    _run_on(x.device, load().quik_linear_w4g, "quik_linear_w4g", args)
+    return y
+
+
+def prepare_linear_w4g(x, w: WeightW4G, bias=None, out=None):
+    """Marshal-once form of quik_linear_w4g: returns (call, y)."""
+    args, y = _linear_w4g_args(x, w, bias, out)
+    return _prepared_on(x.device, load().quik_linear_w4g, "quik_linear_w4g", args, (x, w, bias, y)), y
+
+
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _moe_route_args(logits, top_k, bias, score, groups, topk_groups, group_top, renormalize, scale, out):
+    if score not in _SCORES:
+        raise ValueError(f"score must be one of {sorted(_SCORES)}, got {score!r}")
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+        raise TypeError("logits must be a device tensor")
+    if logits.dim() != 2:
+        raise ValueError("logits must be [tokens, experts]")
+    T, E = logits.shape
+    ldl = _matrix(logits, tuple(_TYPES), "logits", T, E, logits.device)
+    _whole(bias, torch.float32, "bias", (E,), logits.device)
+    if out is None:
+        ids = torch.empty((T, max(top_k, 0)), dtype=torch.int32, device=logits.device)
+        weights = torch.empty((T, max(top_k, 0)), dtype=torch.float32, device=logits.device)
+    else:
+        ids, weights = out
+        if ids is None or weights is None:
+            raise TypeError("out must be (ids, weights)")
+        _whole(ids, torch.int32, "ids", (T, top_k), logits.device)
+        _whole(weights, torch.float32, "weights", (T, top_k), logits.device)
+    return (_TYPES[logits.dtype], _ptr(logits), T, E, ldl, _ptr(bias), _SCORES[score], groups,
+            topk_groups, group_top, top_k, int(bool(renormalize)), float(scale), _ptr(ids), _ptr(weights)), (ids, weights)
+
+
+def quik_moe_route(logits, top_k: int, bias=None, score: str = "softmax", groups: int = 1, topk_groups: int = 1,
+                   group_top: int = 1, renormalize: bool = True, scale: float = 1.0, out=None):
+    """logits fp32, fp16 or bf16 [T, experts] -> (ids int32 [T, top_k], weights fp32 [T, top_k]): the experts of every
+    token, largest first, and what their outputs count.  bias fp32 [experts] is added to the scores for choosing only; of
+    `groups` groups of consecutive experts the topk_groups with the largest sums of group_top scores take part."""
+    args, out = _moe_route_args(logits, top_k, bias, score, groups, topk_groups, group_top, renormalize, scale, out)
+    _run_on(logits.device, load().quik_moe_route, "quik_moe_route", args)
+    return out
+
+
+def prepare_moe_route(logits, top_k: int, bias=None, score: str = "softmax", groups: int = 1, topk_groups: int = 1,
+                      group_top: int = 1, renormalize: bool = True, scale: float = 1.0, out=None):
+    """Marshal-once form of quik_moe_route: returns (call, (ids, weights))."""
+    args, out = _moe_route_args(logits, top_k, bias, score, groups, topk_groups, group_top, renormalize, scale, out)
+    return _prepared_on(logits.device, load().quik_moe_route, "quik_moe_route", args, (logits, bias, out)), out
+
+
+def quik_moe_workspace_bytes(T: int, top_k: int, w: WeightW4G, combine: bool) -> int:
+    """Bytes of the workspace of quik_moe_linear_w4g (combine: with weights)."""
+    return load().quik_moe_workspace_bytes(T, top_k, w.N, int(w.glu), w.experts, int(bool(combine)))
+
+
+def _moe_linear_w4g_args(x, ids, w, weights, bias, out, workspace):
+    _w4g(w, x, experts=True)
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        raise TypeError("ids must be a device tensor [tokens, top_k]")
+    T, top_k = ids.shape
+    _whole(ids, torch.int32, "ids", (T, top_k), x.device)
+    per_slot = x.dim() == 2 and x.shape[0] == T * top_k and x.shape[0] != T
+    ldx = _matrix(x, (torch.float16, torch.bfloat16), "x", T * top_k if per_slot else T, w.K, x.device)
+    _whole(weights, torch.float32, "weights", (T, top_k), x.device)
+    _whole(bias, x.dtype, "bias", (w.experts, w.N), x.device)
+    rows = T if weights is not None else T * top_k
+    y = torch.empty((rows, w.width), dtype=x.dtype, device=x.device) if out is None else out
+    ldy = _matrix(y, (x.dtype,), "out", rows, w.width, x.device)
+    if workspace is None:
+        workspace = torch.empty(quik_moe_workspace_bytes(T, top_k, w, weights is not None), dtype=torch.uint8,
+                                device=x.device)
+    elif not isinstance(workspace, torch.Tensor) or workspace.device != x.device or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous tensor on the device of x")
+    return (_TYPES[x.dtype], _ptr(x), ldx, int(per_slot), _ptr(ids), _ptr(weights), T, top_k, w.K, _ptr(w.data), w.group,
+            int(w.has_zero), int(w.glu), _ptr(bias), w.N, w.experts, _ptr(y), ldy, _ptr(workspace),
+            _nbytes(workspace)), y, workspace
+
+
+def quik_moe_linear_w4g(x, ids, w: WeightW4G, weights=None, bias=None, out=None, workspace=None):
+    """The products of a layer of experts.  ids int32 [T, top_k] (quik_moe_route); x fp16 or bf16, a row per token [T, K]
+    or per slot [T * top_k, K].  Without weights: y [T * top_k, w.width], a row per slot (zeros where the id is no
+    expert).  With weights fp32 [T, top_k]: y [T, w.width], the weighted sum of a token's slots."""
+    args, y, _ = _moe_linear_w4g_args(x, ids, w, weights, bias, out, workspace)
+    _run_on(x.device, load().quik_moe_linear_w4g, "quik_moe_linear_w4g", args)
+    return y
+
+
+def prepare_moe_linear_w4g(x, ids, w: WeightW4G, weights=None, bias=None, out=None, workspace=None):
+    """Marshal-once form of quik_moe_linear_w4g: returns (call, y)."""
+    args, y, workspace = _moe_linear_w4g_args(x, ids, w, weights, bias, out, workspace)
+    return _prepared_on(x.device, load().quik_moe_linear_w4g, "quik_moe_linear_w4g", args,
+                        (x, ids, w, weights, bias, y, workspace)), y

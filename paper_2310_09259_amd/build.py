@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libquik.so")
 SOURCES = ["quik_api.hip", "quik_quantize.hip", "quik_gemm.hip", "quik_gemm_rows.hip", "quik_gemm_tiles16.hip", "quik_gemm_stream.hip", "quik_gemm_fp6.hip", "quik_gemm_sp24.hip",
-           "quik_unfused.hip", "quik_probe.hip"]
+           "quik_unfused.hip", "quik_probe.hip", "quik_w4g.hip", "quik_moe.hip", "quik_w4g_api.hip"]
 
 CALL_SRC, CALL_LIB = os.path.join(CSRC, "quik_call.cpp"), os.path.join(HERE, "_quik_call.so")
 

@@ -1,0 +1,51 @@
+// Launch interfaces of the layers with 4-bit weights in groups and of the layers of experts (quik_w4g_api.hip is their
+// C boundary).  Private to the shared library.
+#pragma once
+#include "quik_w4g_device.h"
+
+namespace quik {
+
+// One product of activations with w4g weights; `rows` rows of output before they are combined.
+struct W4gArgs {
+    const void* x;                // 16 bits [.., ldx]
+    int ldx;
+    w4g::Weights w;
+    int group;                    // columns of a stored group: 32, 64 or 128
+    int bf16, glu;                // type of x, bias and y; paired halves
+    const void* bias;             // [E][N] or null
+    void* y;                      // [.., ldy]
+    int ldy;
+    int width;                    // columns of y: N, or N / 2 for paired halves
+    int rows;                     // dense: tokens; experts: T * top_k
+    // experts only (ids == null: dense)
+    const int32_t* ids;           // [rows]
+    int experts, top_k;
+    int x_per_slot;               // row r of x is r, else r / top_k
+    int32_t* plan;                // room for launch_moe_plan's, which launch_w4g makes where it uses one
+    const float* weights;         // [rows]: y is [T], the weighted sum of a token's slots; or null: y is [rows]
+    float* stage;                 // [rows][width] for the sum, where the rows are computed one by one
+};
+hipError_t launch_w4g(const W4gArgs& a, hipStream_t stream);
+hipError_t launch_weight_pack_w4g(const void* w_q, int ldw, const void* w_scale, const void* w_zero, int N, int K, int group,
+                                  int glu, int experts, void* w4, hipStream_t stream);
+
+// plan: int32 [experts + 2 + rows]: first row of every expert, the number of rows that have one, the number of rows; then
+// the rows, ordered by expert, those of no expert last, in ascending order each
+hipError_t launch_moe_plan(const int32_t* ids, int rows, int experts, int32_t* plan, hipStream_t stream);
+hipError_t launch_moe_combine(const float* stage, const int32_t* ids, const float* weights, int T, int top_k, int experts,
+                              int width, int bf16, void* y, int ldy, hipStream_t stream);
+
+struct MoeRouteArgs {
+    const void* logits;           // [T, ldl]
+    int type;                     // QUIK_F16, QUIK_BF16, QUIK_F32
+    int T, E, ldl;
+    const float* bias;            // [E] or null
+    int sigmoid;                  // else softmax
+    int groups, topk_groups, group_top, top_k, renormalize;
+    float scale;
+    int32_t* ids;                 // [T, top_k]
+    float* weights;               // [T, top_k]
+};
+hipError_t launch_moe_route(const MoeRouteArgs& a, hipStream_t stream);
+
+}  // namespace quik
