@@ -497,8 +497,8 @@ int quik_linear_sp24(const void *x, int T, int K, int ldx, const int32_t *outlie
  *                         those that w4 was packed with.  One kernel launch, no workspace.
  *
  * Limits of these layers: T >= 1; K a multiple of 8, at most 32768; N at most 2^20; x and w4 16-byte aligned, ldx a
- * multiple of 8; ldy >= the columns of y, y otherwise unconstrained; w_q 16-byte aligned, ldw a multiple of 16.  y does not
- * overlap an input.
+ * multiple of 8, at most 2^22; scales and zero points of a layer (of all its experts) below 3.75 GB; ldy >= the columns of
+ * y, y otherwise unconstrained; w_q 16-byte aligned, ldw a multiple of 16.  y does not overlap an input.
  */
 size_t quik_w4g_bytes(int N, int K, int group, int has_zero, int glu, int experts);
 int quik_weight_pack_w4g(const void *w_q, int ldw, const void *w_scale, const void *w_zero, int N, int K, int group, int glu,
@@ -533,7 +533,7 @@ int quik_linear_w4g(int type, const void *x, int T, int K, int ldx, const void *
  *      bias        [experts, N] or NULL
  *      workspace   quik_moe_workspace_bytes(T, top_k, N, glu, experts, weights != NULL) bytes, 256-byte aligned; nothing
  *                  has to be cleared, nothing is kept; calls that may overlap in time need one each
- *    Limits: those of the w4g layers; T * top_k <= 2^24.
+ *    Limits: those of the w4g layers; T * top_k <= 2^24; x below 3.75 GB.
  */
 int quik_moe_route(int type, const void *logits, int T, int experts, int ldl, const float *bias, int score, int groups,
                    int topk_groups, int group_top, int top_k, int renormalize, float scale, int32_t *ids, float *weights,
@@ -542,6 +542,17 @@ size_t quik_moe_workspace_bytes(int T, int top_k, int N, int glu, int experts, i
 int quik_moe_linear_w4g(int type, const void *x, int ldx, int x_per_slot, const int32_t *ids, const float *weights, int T,
                         int top_k, int K, const void *w4, int group, int has_zero, int glu, const void *bias, int N,
                         int experts, void *y, int ldy, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Test hooks of these products (host only).  quik_debug_w4g_form: the kernel that a product of `rows` rows (experts: T *
+ * top_k; 0 experts: a layer) runs on with `cus` compute units: 0 .. 5 the kernels whose waves split K, of 16 x 16,
+ * 16 x 32 (eight waves), 16 x 32 (four), 16 x 64, 32 x 32 and 32 x 64 rows x channels; 6 .. 10 the tile kernels of 32 x 128,
+ * 64 x 128, 128 x 128, 256 x 128 and 256 x 256.  QUIK_EINVAL / QUIK_EUNSUPPORTED on invalid input.
+ * quik_debug_set_w4g_form: the one that products use from now on, in this process, where they can; -1: automatic.  Not
+ * synchronised with calls in flight on other threads.
+ */
+int quik_debug_w4g_form(int rows, int N, int K, int glu, int experts, int cus);
+int quik_debug_set_w4g_form(int form);
 
 /*
  * Measurement probes (not part of the layer): what the chip sustains, so that a kernel's rate can

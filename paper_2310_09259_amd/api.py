@@ -126,6 +126,10 @@ def load() -> C.CDLL:
         lib.quik_weight_pack_w4g.argtypes = [vp, i, vp, vp, i, i, i, i, i, vp, vp]
         lib.quik_linear_w4g.restype = i
         lib.quik_linear_w4g.argtypes = [i, vp, i, i, i, vp, i, i, i, vp, i, vp, i, vp]
+        lib.quik_debug_w4g_form.restype = i
+        lib.quik_debug_w4g_form.argtypes = [i, i, i, i, i, i]
+        lib.quik_debug_set_w4g_form.restype = i
+        lib.quik_debug_set_w4g_form.argtypes = [i]
         lib.quik_moe_route.restype = i
         lib.quik_moe_route.argtypes = [i, vp, i, i, i, vp, i, i, i, i, i, i, C.c_float, vp, vp, vp]
         lib.quik_moe_workspace_bytes.restype = C.c_size_t
@@ -1051,6 +1055,19 @@ def prepare_linear_w4g(x, w: WeightW4G, bias=None, out=None):
     """Marshal-once form of quik_linear_w4g: returns (call, y)."""
     args, y = _linear_w4g_args(x, w, bias, out)
     return _prepared_on(x.device, load().quik_linear_w4g, "quik_linear_w4g", args, (x, w, bias, y)), y
+
+
+def quik_debug_w4g_form(rows: int, N: int, K: int, glu: bool = False, experts: int = 0, cus: int = 256) -> int:
+    """Host-only: the kernel (see include/quik.h) of a w4g product of this many rows on `cus` compute units."""
+    form = load().quik_debug_w4g_form(rows, N, K, int(glu), experts, cus)
+    if form < 0:
+        _check(form, "quik_debug_w4g_form")
+    return form
+
+
+def quik_debug_set_w4g_form(form: int):
+    """-1 automatic, else the kernel that w4g products use where they can."""
+    _check(load().quik_debug_set_w4g_form(form), "quik_debug_set_w4g_form")
 
 
 _SCORES = {"softmax": 0, "sigmoid": 1}

@@ -1,10 +1,15 @@
 // Products with 4-bit weights in groups (layout: quik_w4g_device.h): y[t, n] = sum_k x[t, k] s[n, k / g] (q[n, k] -
 // z[n, k / g]), for a dense layer and for the experts that a router chose.
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "quik_gemm_device.h"
+#include "quik_kernels.h"
 #include "quik_w4g.h"
+#include "quik_w4g_rows_device.h"
 
 namespace quik {
 
@@ -57,125 +62,274 @@ __global__ __launch_bounds__(256) void pack_w4g_kernel(PackArgs a) {
     }
 }
 
-// ---- sixteen rows at a time
+// ---- few rows: the waves of a workgroup split K
+//
+// What bounds it: up to some 32 rows the weights, read once; beyond that the activations, which every workgroup reads whole
+// out of L2.  A wave copies its tiles of 128 columns global -> LDS into a private ring of NST stages (no barrier until the
+// waves add up), weights with the hint that they are read once: whole tiles of 1 KB, the row blocks' activations in
+// pieces of 256 bytes a row, a channel block's scales and zero points in one copy.  (Activations loaded straight into
+// registers as the matrix instructions want them, neighbouring lanes in different rows, take a clock of the CU's address
+// path per lane: 64 x 16384 x 11008 came to 72 us that way, whatever the blocks.)
+// A group's sum of x (q - z) is exact in its operands (16-bit activations, integers of at most eight bits) and held in
+// fp32, and the scale is applied to it in fp32.  fp16 subtracts offset and zero point from the codes before the product;
+// bf16, which has no packed subtraction, multiplies the codes with their offset of 128 and takes 136 + z times the sum
+// of x off afterwards (an operand of ones gives it in the layout of the accumulators).
+// Waves add up through LDS in wave order.
+//
+// MB, CB: row blocks and channel blocks of 16; NW waves.
+// Rows of a block: consecutive ones (dense), those of a block of the plan, or one (a row at a time).  TOKEN: with weights and
+// no plan a workgroup takes a token: the columns of its slots follow each other as if they were one long row, each slot's
+// scales multiplied by its weight.
+template <typename TY, int KG, int MB, int CB, int NW, int NST, bool TOKEN>
+// (the bound, of more threads than a launch has, keeps the compiler to 256 registers where LDS would allow it more)
+__global__ __launch_bounds__(512) void w4g_rows_kernel(W4gArgs a, int groups_n) {
+    constexpr int PER = kCols / KG;
+    constexpr bool SUMS = TY::kOffset < 1000.0f;
+    constexpr int X_BYTES = MB * 16 * 256, S_AT = X_BYTES + CB * kTileBytes, STAGE = S_AT + CB * 256;
+    constexpr int X_COPIES = MB * 4, LPS = X_COPIES + 2 * CB;
+    static_assert((NST - 1) * LPS < 64, "vmcnt range");
+    constexpr int RING = NW * NST * STAGE, RED = NW * MB * CB * 1024;
+    if constexpr (MB * CB > 2) asm volatile("" ::: "v255");   // a whole share of the register file (see quik_gemm.hip)
+    else asm volatile("" ::: "v127");
+    __shared__ __align__(1024) uint8_t lds[RING > RED ? RING : RED];     // rings; then the partial sums
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
+    const int id = gemm_dev::xcd_contiguous_id(blockIdx.x, gridDim.x);
+    const int b0 = id % groups_n * CB, block = id / groups_n;
 
-struct RowSource {                   // what a workgroup's sixteen rows are
-    int expert;                      // -1: none, the rows are zeros
-    int first, count;                // rows first .. first + count - 1 of the list, or of the output
-    bool listed;                     // through plan's list
-};
-
-// the sixteen rows of block b of a plan: blocks of an expert's rows follow each other, then those of no expert
-__device__ __forceinline__ RowSource planned_rows(const int32_t* plan, int experts, int b, int bm) {
-    RowSource r{-1, 0, 0, true};
-    for (int e = 0; e <= experts; ++e) {
-        const int at = plan[e], blocks = (plan[e + 1] - at + bm - 1) / bm;
-        if (b < blocks) {
-            r.expert = e < experts ? e : -1;
-            r.first = at + b * bm;
-            r.count = min(bm, plan[e + 1] - r.first);
-            return r;
-        }
-        b -= blocks;
-    }
-    return r;
-}
-
-// Four waves split K; the wave's partial sums are added in wave order.  A group's sum of x (q - z) is exact in its
-// operands (16-bit activations, integers of at most eight bits) and held in fp32, and the scale is applied to it in fp32.
-template <typename TY, int KG>
-__global__ __launch_bounds__(256) void w4g_rows_kernel(W4gArgs a) {
-    constexpr int NW = 4, CB = 2, PER = kCols / KG;
-    __shared__ float red[NW][CB][64][4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
-    const int b0 = blockIdx.x * CB;
-
-    RowSource src{0, (int)blockIdx.y * 16, min(16, a.rows - (int)blockIdx.y * 16), false};
-    if (a.ids && a.plan) {
-        src = planned_rows(a.plan, a.experts, blockIdx.y, 16);
+    RowSource src{0, block * MB * 16, min(MB * 16, a.rows - block * MB * 16), false};
+    if (!TOKEN && a.plan) {
+        src = planned_rows(a.plan, a.experts, block, MB * 16);
         if (src.count == 0) return;
+    } else if (TOKEN) {
+        src = RowSource{0, block, 1, false};
     } else if (a.ids) {
-        const int e = a.ids[blockIdx.y];
-        src = RowSource{e >= 0 && e < a.experts ? e : -1, (int)blockIdx.y, 1, false};
+        const int e = a.ids[block];
+        src = RowSource{e >= 0 && e < a.experts ? e : -1, block, 1, false};
     }
-    const int32_t* list = src.listed ? a.plan + a.experts + 2 + src.first : nullptr;
+    const int32_t* const list = src.listed ? a.plan + a.experts + 2 + src.first : nullptr;
 
-    v4f acc[CB] = {};
-    if (src.expert >= 0) {
-        const uint8_t* codes = a.w.codes + src.expert * a.w.codes_e;
-        const uint16_t* scales = reinterpret_cast<const uint16_t*>(a.w.scales + src.expert * a.w.scales_e);
-        const int8_t* zeros = a.w.zeros ? reinterpret_cast<const int8_t*>(a.w.zeros + src.expert * a.w.zeros_e) : nullptr;
-        const bool row_ok = l16 < src.count;
-        int row = row_ok ? (list ? list[l16] : src.first + l16) : 0;
-        if (a.ids && !a.x_per_slot) row /= a.top_k;
-        const uint16_t* x = static_cast<const uint16_t*>(a.x) + (size_t)row * a.ldx;
-        const v4u ones = v4u{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-        for (int kt = a.w.kt * wave / NW; kt < a.w.kt * (wave + 1) / NW; ++kt) {
-            v4u xa[4];
+    // ---- where this lane's copies come from.  x: by offsets from the first row (dense) or from x; copy i brings rows
+    // 4 i .. 4 i + 3, its piece p of a row into place p ^ (row % 16), and zeros beyond the rows or beyond K
+    const uint8_t* xbase = static_cast<const uint8_t*>(a.x);
+    if (!a.ids) xbase += (size_t)src.first * a.ldx * 2;
+    else if (!list) xbase += (size_t)(TOKEN ? (a.x_per_slot ? block * a.top_k : block)
+                                            : (a.x_per_slot ? block : block / a.top_k)) * a.ldx * 2;
+    const gemm_dev::v4i rx = whole_rsrc(xbase);
+    uint32_t vo[X_COPIES];
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int k = kt * kCols + s * 32 + g * 8;
-                xa[s] = row_ok && k < a.w.K ? *reinterpret_cast<const v4u*>(x + k) : v4u{0, 0, 0, 0};
-            }
+    for (int i = 0; i < X_COPIES; ++i) {
+        const int r = 4 * i + g;
+        uint32_t row = list ? 0 : r;
+        if (list && r < src.count) row = (uint32_t)list[r] / (a.x_per_slot ? 1u : (uint32_t)a.top_k);
+        vo[i] = r < src.count ? row * (uint32_t)(a.ldx * 2) + ((l16 ^ (r & 15)) << 4) : kBeyond;
+    }
+    // a block's scales in the first 128 bytes of its 256, its zero points (or zeros) in the second
+    const size_t tile0 = (size_t)b0 * a.w.kt;
+    const bool is_scale = lane < 8 * PER, is_zero = a.w.zeros && lane >= 32 && lane < 32 + 4 * PER;
+    const uint32_t per_tile = is_zero ? kBlock * PER : kBlock * PER * 2;
+
+    uint8_t* const ring = lds + wave * (NST * STAGE);
+    const uint32_t ring_addr = gemm_dev::lds_addr(ring);
+    const int tiles = src.expert < 0 ? 0 : TOKEN ? a.top_k * a.w.kt : a.w.kt;
+    const int first = tiles * wave / NW, last = tiles * (wave + 1) / NW;
+    // tile vt of this wave's range, or past its end the last one again -> the weight of its slot
+    auto issue = [&](int vt, int slot) {
+        vt = min(vt, last - 1);
+        int kt = vt, e = src.expert, room = a.w.K;
+        uint32_t at = 0;
+        float weight = 1.0f;
+        if constexpr (TOKEN) {
+            const int j = vt / a.w.kt, r = block * a.top_k + j;
+            kt = vt - j * a.w.kt;
+            e = a.ids[r];
+            const bool on = e >= 0 && e < a.experts;
+            e = on ? e : 0;
+            const float v = a.weights[r];
+            weight = on ? v : 0.0f;
+            room = on ? room : 0;
+            at = (uint32_t)(a.x_per_slot ? j : 0) * (uint32_t)(a.ldx * 2);
+        }
+        room -= kt * kCols;
+        at += (uint32_t)kt * 256;
+        const uint32_t dst = ring_addr + slot * STAGE;
+        const gemm_dev::v4i rw = whole_rsrc(a.w.codes + e * a.w.codes_e + tile0 * kTileBytes);
+        const uint8_t* const s0 = a.w.scales + e * a.w.scales_e + tile0 * (kBlock * PER * 2);
+        const gemm_dev::v4i rs = whole_rsrc(s0);
+        const uint32_t zeros_at = a.w.zeros ? (uint32_t)(a.w.zeros + e * a.w.zeros_e + tile0 * (kBlock * PER) - s0) : 0u;
+        const uint32_t so = is_zero ? zeros_at + (lane - 32) * 4 : lane * 4;
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+            const uint32_t tile = (uint32_t)min(c, a.w.nt - 1 - b0) * a.w.kt + kt;
+            gemm_dev::dma16_once(rw, dst + X_BYTES + c * kTileBytes, lane * 16 + tile * kTileBytes);
+            gemm_dev::dma4(rs, dst + S_AT + c * 256, is_scale || is_zero ? so + tile * per_tile : kBeyond);
+        }
+#pragma unroll
+        for (int i = 0; i < X_COPIES; ++i)
+            gemm_dev::dma16(rx, dst + i * 1024, (l16 ^ ((4 * i + g) & 15)) * 8 < room ? vo[i] : kBeyond, at);
+        return weight;
+    };
+
+    v4f acc[MB][CB] = {};
+    const v4u ones = v4u{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+    uint32_t mask = 0x000F000Fu, bits = TY::kBits;       // (in registers: two literals would cost an instruction more)
+    asm volatile("" : "+s"(mask), "+v"(bits));
+    auto multiply = [&](const uint8_t* st, float weight) {
+        v4u w[CB];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) w[c] = *reinterpret_cast<const v4u*>(st + X_BYTES + c * kTileBytes + lane * 16);
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            v4f part[MB][CB] = {}, sum[MB] = {};
+            int zero[CB];
+            float scale[CB];
 #pragma unroll
             for (int c = 0; c < CB; ++c) {
-                if (b0 + c >= a.w.nt) continue;
-                const size_t tile = (size_t)(b0 + c) * a.w.kt + kt;
-                const v4u w = *reinterpret_cast<const v4u*>(codes + tile * kTileBytes + lane * 16);
+                const uint8_t* const sz = st + S_AT + c * 256 + l16 * PER + p;
+                scale[c] = (float)*reinterpret_cast<const _Float16*>(st + S_AT + c * 256 + (l16 * PER + p) * 2);
+                if constexpr (TOKEN) scale[c] *= weight;
+                zero[c] = (int)(8.0f + TY::kOffset) + *reinterpret_cast<const int8_t*>(sz + 128);
+            }
 #pragma unroll
-                for (int p = 0; p < PER; ++p) {
-                    const size_t at = (tile * 16 + l16) * PER + p;
-                    const float scale = (float)__builtin_bit_cast(_Float16, scales[at]);
-                    const float zero = 8.0f + TY::kOffset + (zeros ? (float)zeros[at] : 0.0f);
-                    v4f part = {}, sum = {};
+            for (int s = p * (4 / PER); s < (p + 1) * (4 / PER); ++s) {
+                v4u x[MB];
 #pragma unroll
-                    for (int s = p * (4 / PER); s < (p + 1) * (4 / PER); ++s) {
-                        v4u b;
+                for (int m = 0; m < MB; ++m)
+                    x[m] = *reinterpret_cast<const v4u*>(st + (m * 16 + l16) * 256 + (((s * 4 + g) ^ l16) << 4));
+                if constexpr (SUMS) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) b[i] = ((w[s] >> (4 * i)) & 0x000F000Fu) | TY::kBits;
-                        if constexpr (TY::kOffset > 1000.0f) {
-                            const v2h z = v2h{(_Float16)zero, (_Float16)zero};
+                    for (int m = 0; m < MB; ++m) sum[m] = TY::mfma(x[m], ones, sum[m]);
+                }
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) b[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, (uint32_t)b[i]) - z);
-                        } else {
-                            sum = TY::mfma(xa[s], ones, sum);
-                        }
-                        part = TY::mfma(xa[s], b, part);
+                for (int c = 0; c < CB; ++c) {
+                    const _Float16 z1 = (_Float16)(short)zero[c];
+                    const v2h z2 = v2h{z1, z1};
+                    v4u b;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t u = ((w[c][s] >> (4 * i)) & mask) | bits;
+                        b[i] = SUMS ? u : __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, u) - z2);
                     }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float v = part[r];
-                        if constexpr (TY::kOffset < 1000.0f) v = __builtin_fmaf(-zero, sum[r], v);
-                        acc[c][r] = __builtin_fmaf(scale, v, acc[c][r]);
-                    }
+                    for (int m = 0; m < MB; ++m) part[m][c] = TY::mfma(x[m], b, part[m][c]);
                 }
             }
+#pragma unroll
+            for (int m = 0; m < MB; ++m)
+#pragma unroll
+                for (int c = 0; c < CB; ++c)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float v = part[m][c][r];
+                        if constexpr (SUMS) v = __builtin_fmaf(-(float)zero[c], sum[m][r], v);
+                        acc[m][c][r] = __builtin_fmaf(scale[c], v, acc[m][c][r]);
+                    }
+        }
+    };
+
+    if (first < last) {
+        float ahead[NST - 1];                            // the weights of the tiles under way
+#pragma unroll
+        for (int d = 0; d < NST - 1; ++d) ahead[d] = issue(first + d, d);
+        int slot = 0, fill = NST - 1;
+        for (int vt = first; vt < last; ++vt) {
+            __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): the reads of the stage about to be filled are done
+            const float next = issue(vt + NST - 1, fill);
+            gemm_dev::wait_vm<(NST - 1) * LPS>();        // tile vt has landed (this wave's own copies)
+            asm volatile("" ::: "memory");
+            multiply(ring + slot * STAGE, ahead[0]);
+#pragma unroll
+            for (int d = 0; d < NST - 2; ++d) ahead[d] = ahead[d + 1];
+            ahead[NST - 2] = next;
+            slot = slot + 1 == NST ? 0 : slot + 1;
+            fill = fill + 1 == NST ? 0 : fill + 1;
+        }
+        gemm_dev::wait_vm<0>();
+    }
+    __syncthreads();                                     // every ring is dead
+    float4 (*red)[MB * CB][64] = reinterpret_cast<float4 (*)[MB * CB][64]>(lds);
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) red[wave][m * CB + c][lane] = make_float4(acc[m][c][0], acc[m][c][1], acc[m][c][2], acc[m][c][3]);
+    __syncthreads();
+
+    // ---- the sums in wave order: a wave finishes a block, or both halves of a pair, and then the next
+    const int step = a.glu ? 2 : 1;
+    for (int q = wave * step; q < MB * CB; q += NW * step) {
+        const int m = q / CB, c = q % CB;
+        const int n = (a.glu ? (b0 + c) >> 1 : b0 + c) * kBlock + l16;
+        if (n >= a.width || m * 16 >= src.count) continue;
+        float v[2][4] = {};
+        for (int h = 0; h < step; ++h) {
+            for (int w = 0; w < NW; ++w) {
+                const float4 f = red[w][q + h][lane];
+                v[h][0] += f.x; v[h][1] += f.y; v[h][2] += f.z; v[h][3] += f.w;
+            }
+            if (a.bias) {
+                float bias = 0.0f;
+                if (TOKEN) {
+                    for (int j = 0; j < a.top_k; ++j) {
+                        const int e = a.ids[block * a.top_k + j];
+                        if (e >= 0 && e < a.experts) bias = __builtin_fmaf(a.weights[block * a.top_k + j], TY::load(a.bias, (size_t)e * a.w.N + n), bias);
+                    }
+                } else if (src.expert >= 0) {
+                    bias = TY::load(a.bias, (size_t)src.expert * a.w.N + n + h * a.width);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[h][r] += bias;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = m * 16 + 4 * g + r;
+            if (i >= src.count) continue;
+            const float y = src.expert < 0 ? 0.0f : a.glu ? silu_product(v[0][r], v[1][r]) : v[0][r];
+            const size_t row = list ? (size_t)list[i] : (size_t)src.first + i;
+            if (a.weights && !TOKEN) a.stage[row * a.width + n] = y;
+            else static_cast<uint16_t*>(a.y)[row * a.ldy + n] = TY::round(y);
         }
     }
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) red[wave][c][lane][r] = acc[c][r];
-    __syncthreads();
-    // wave c finishes block c of the two, or wave 0 both halves of a pair
-    if (wave >= (a.glu ? 1 : CB)) return;
-    const int n = a.glu ? (b0 >> 1) * kBlock + l16 : (b0 + wave) * kBlock + l16;
-    if (n >= a.width) return;
-    const size_t bias_at = (size_t)(src.expert > 0 ? src.expert : 0) * a.w.N;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int i = 4 * g + r;
-        if (i >= src.count) continue;
-        float v[2] = {0.0f, 0.0f};
-        for (int h = 0; h < (a.glu ? 2 : 1); ++h) {
-            for (int w = 0; w < NW; ++w) v[h] += red[w][a.glu ? h : wave][lane][r];
-            if (a.bias && src.expert >= 0) v[h] += TY::load(a.bias, bias_at + n + h * a.width);
+}
+
+template <typename TY, int KG, int MB, int CB, int NW, int NST>
+hipError_t launch_rows(const W4gArgs& a, hipStream_t stream) {
+    const int groups_n = (a.w.nt + CB - 1) / CB;
+    const dim3 threads(NW * 64);
+    if constexpr (MB == 1) {
+        if (a.weights && !a.plan && !a.glu) {
+            hipLaunchKernelGGL((w4g_rows_kernel<TY, KG, 1, CB, NW, NST, true>), dim3((unsigned)(a.rows / a.top_k) * groups_n), threads, 0, stream, a, groups_n);
+            return hipGetLastError();
         }
-        if (a.glu) v[0] = silu_product(v[0], v[1]);
-        const size_t row = list ? list[i] : src.first + i;
-        if (src.expert < 0) v[0] = 0.0f;
-        if (a.weights) a.stage[row * a.width + n] = v[0];
-        else static_cast<uint16_t*>(a.y)[row * a.ldy + n] = TY::round(v[0]);
+    }
+    int blocks = (a.rows + MB * 16 - 1) / (MB * 16);
+    if (a.plan) blocks = a.rows / (MB * 16) + min(a.rows, a.experts + 1);
+    else if (a.ids) blocks = a.rows;
+    hipLaunchKernelGGL((w4g_rows_kernel<TY, KG, MB, CB, NW, NST, false>), dim3((unsigned)blocks * groups_n), threads, 0, stream, a, groups_n);
+    return hipGetLastError();
+}
+
+template <typename TY, int KG>
+hipError_t rows_dispatch(const W4gArgs& a, int form, hipStream_t stream) {
+    switch (form) {
+        case kW4gRows16x16: return launch_rows<TY, KG, 1, 1, 8, 3>(a, stream);
+        case kW4gRows16x32Wide: return launch_rows<TY, KG, 1, 2, 8, 2>(a, stream);
+        case kW4gRows16x32: return launch_rows<TY, KG, 1, 2, 4, 2>(a, stream);
+        case kW4gRows16x64: return launch_rows<TY, KG, 1, 4, 4, 2>(a, stream);
+        case kW4gRows32x32: return launch_rows<TY, KG, 2, 2, 6, 2>(a, stream);
+        case kW4gRows32x64: return launch_rows<TY, KG, 2, 4, 6, 2>(a, stream);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+hipError_t launch_w4g_rows(const W4gArgs& a, int form, hipStream_t stream) {
+    switch (a.group + a.bf16) {
+        case 32: return rows_dispatch<Half, 32>(a, form, stream);
+        case 64: return rows_dispatch<Half, 64>(a, form, stream);
+        case 128: return rows_dispatch<Half, 128>(a, form, stream);
+        case 33: return rows_dispatch<Bf16, 32>(a, form, stream);
+        case 65: return rows_dispatch<Bf16, 64>(a, form, stream);
+        case 129: return rows_dispatch<Bf16, 128>(a, form, stream);
+        default: return hipErrorInvalidValue;
     }
 }
 
@@ -193,26 +347,62 @@ hipError_t launch_weight_pack_w4g(const void* w_q, int ldw, const void* w_scale,
     return hipGetLastError();
 }
 
+namespace { std::atomic<int> g_form{-1}; }
+void set_w4g_form(int form) { g_form.store(form, std::memory_order_relaxed); }
+
+// Up to 16 rows the choice goes by the channel blocks of all rows together (us, weights from HBM, K = 4096 unless noted):
+//  - one block per CU or fewer: single blocks and eight waves (N = 4096, 1 row: 6.0 against 6.7 with pairs, 7.4 with four
+//    waves); paired halves, and up to two per CU: pairs and eight waves;
+//  - more: pairs and four waves, two and three workgroups to a CU (N = 15360, K = 5120: 11.4 against 13.8 with eight waves);
+//    from six blocks per CU on four of them at a time (N = 28672, K = 8192: 24.9 against 26.9).
+// Above that the least of an estimate: rounds of workgroups, one to a CU, times the tiles of 128 columns that a wave (or
+// group of waves) goes through, times what such a step takes, plus a start.  Measured steps: 1.3 us and 1.75 for 32 x 32 and 32 x 64
+// (six waves split K), 0.95 and 1.3 for tiles of 32 x 128 and 64 x 128 (two groups split K), 1.2, 2.1 and 3.3 for
+// 128 x 128, 256 x 128 and 256 x 256.  N = 11008, chosen : best other one: 32 rows 13.5 : 17.3, 64 rows 17.9 : 23.6, 128 rows 23.3 : 33.7,
+// 256 rows 40 : 46, 512 rows 61 : 81, 1024 rows 102 : 128, 2048 rows 209 : 215; N = 4096, 256 rows 20.6 : 25;
+// N = 28672, K = 8192, 4096 rows 1630 : 1930.
+// Experts: the rows spread over all of them, each with half a tile to spare.
+int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, int cus) {
+    const double active = experts ? min(rows, experts) : 0;
+    if (by_rows || (experts ? rows <= 4 * active : rows <= 16)) {
+        const double all = (double)blocks * (by_rows ? rows : experts ? active : 1);
+        if (all <= cus && !glu) return kW4gRows16x16;
+        if (all <= 2 * cus) return kW4gRows16x32Wide;
+        return all >= 6 * cus ? kW4gRows16x64 : kW4gRows16x32;
+    }
+    struct Cost { int form, rows, blocks, k_split; double start, step; };
+    static const Cost costs[] = {
+        {kW4gRows32x32, 32, 2, 6, 5.0, 1.3},     {kW4gRows32x64, 32, 4, 6, 5.0, 1.75},    {kW4gTile32x128, 32, 8, 2, 3.0, 0.95},
+        {kW4gTile64x128, 64, 8, 2, 3.0, 1.3},    {kW4gTile128x128, 128, 8, 1, 3.0, 1.2},  {kW4gTile256x128, 256, 8, 1, 3.0, 2.1},
+        {kW4gTile256x256, 256, 16, 1, 3.0, 3.3},
+    };
+    int best = kW4gTile256x256;
+    double least = 1e30;
+    for (const Cost& c : costs) {
+        double tiles = (rows + c.rows - 1) / c.rows;
+        if (experts) tiles = (double)rows / c.rows + active / 2 > active ? (double)rows / c.rows + active / 2 : active;
+        tiles *= (blocks + c.blocks - 1) / c.blocks;
+        const double t = c.start + ceil(tiles / cus) * ((kt + c.k_split - 1) / c.k_split) * c.step;
+        if (t < least) { least = t; best = c.form; }
+    }
+    return best;
+}
+
 hipError_t launch_w4g(const W4gArgs& args, hipStream_t stream) {
     W4gArgs a = args;
-    int blocks = (a.rows + 15) / 16;
-    if (a.ids) {
-        if (a.rows <= a.experts) a.plan = nullptr;       // a row at a time: hardly two share an expert
-        else if (hipError_t rc = launch_moe_plan(a.ids, a.rows, a.experts, a.plan, stream); rc != hipSuccess) return rc;
-        blocks = a.plan ? (a.rows + 15) / 16 + min(a.rows, a.experts + 1) : a.rows;
+    // a row (or a token and its slots) at a time where hardly two rows share an expert: no plan, no sums in memory
+    const bool by_rows = a.ids && a.rows <= a.experts;
+    if (by_rows) a.plan = nullptr;
+    else if (a.ids) {
+        if (hipError_t rc = launch_moe_plan(a.ids, a.rows, a.experts, a.plan, stream); rc != hipSuccess) return rc;
     }
-    const dim3 grid((a.w.nt + 1) / 2, blocks), threads(256);
-    switch (a.group + a.bf16) {
-        case 32: hipLaunchKernelGGL((w4g_rows_kernel<Half, 32>), grid, threads, 0, stream, a); break;
-        case 64: hipLaunchKernelGGL((w4g_rows_kernel<Half, 64>), grid, threads, 0, stream, a); break;
-        case 128: hipLaunchKernelGGL((w4g_rows_kernel<Half, 128>), grid, threads, 0, stream, a); break;
-        case 33: hipLaunchKernelGGL((w4g_rows_kernel<Bf16, 32>), grid, threads, 0, stream, a); break;
-        case 65: hipLaunchKernelGGL((w4g_rows_kernel<Bf16, 64>), grid, threads, 0, stream, a); break;
-        case 129: hipLaunchKernelGGL((w4g_rows_kernel<Bf16, 128>), grid, threads, 0, stream, a); break;
-        default: return hipErrorInvalidValue;
-    }
-    hipError_t rc = hipGetLastError();
-    if (rc != hipSuccess || !a.weights) return rc;
+    const int cus = compute_units();
+    int form = g_form.load(std::memory_order_relaxed);
+    if (form < 0) form = choose_w4g_form(a.rows, a.w.nt, a.w.kt, a.glu, a.ids ? a.experts : 0, by_rows, cus > 0 ? cus : 256);
+    if (by_rows && form > kW4gRows16x64) form = kW4gRows16x32;
+    if (a.glu && form == kW4gRows16x16) form = kW4gRows16x32Wide;
+    const hipError_t rc = form < kW4gTile32x128 ? launch_w4g_rows(a, form, stream) : launch_w4g_tiles(a, form, stream);
+    if (rc != hipSuccess || !a.weights || (by_rows && !a.glu)) return rc;
     return launch_moe_combine(a.stage, a.ids, a.weights, a.rows / a.top_k, a.top_k, a.experts, a.width, a.bf16, a.y, a.ldy, stream);
 }
 

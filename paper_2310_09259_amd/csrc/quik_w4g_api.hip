@@ -10,6 +10,9 @@ namespace {
 
 constexpr int kMaxK = 32768, kMaxN = 1 << 20, kMaxTokens = 1 << 24, kMaxRows = 1 << 24, kMaxExperts = 1024, kMaxTopK = 32,
               kMaxGroups = 64;
+// the kernels address x from a tile's first row (experts: from its start), and scales and zero points, by 32-bit offsets
+constexpr int kMaxLdx = 1 << 22;
+constexpr size_t kMaxOffset = 0xF0000000u;
 
 inline bool aligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 inline int status(hipError_t rc) { return rc == hipSuccess ? QUIK_OK : QUIK_ELAUNCH; }
@@ -30,7 +33,9 @@ int check_product(int type, const void* x, int T, int K, int ldx, const void* w4
     if ((type != QUIK_F16 && type != QUIK_BF16) || (has_zero != 0 && has_zero != 1)) return QUIK_EINVAL;
     if (T <= 0 || ldx < K || ldy < (glu ? N / 2 : N)) return QUIK_EINVAL;
     if (!x || !w4 || !y) return QUIK_ENULL;
-    if (T > kMaxTokens) return QUIK_EUNSUPPORTED;
+    if (T > kMaxTokens || ldx > kMaxLdx) return QUIK_EUNSUPPORTED;
+    const quik::w4g::Layout l = quik::w4g::layout(N, K, group, has_zero != 0, glu != 0, experts);
+    if (l.total - l.scales_at > kMaxOffset) return QUIK_EUNSUPPORTED;
     if (ldx % 8 || !aligned(x, 16) || !aligned(w4, 16) || !aligned(y, 2) || !aligned(bias, 2)) return QUIK_EALIGN;
     return QUIK_OK;
 }
@@ -91,6 +96,20 @@ int quik_linear_w4g(int type, const void* x, int T, int K, int ldx, const void* 
     return status(quik::launch_w4g(a, static_cast<hipStream_t>(stream)));
 }
 
+int quik_debug_w4g_form(int rows, int N, int K, int glu, int experts, int cus) {
+    if (rows <= 0 || experts < 0 || cus <= 0) return QUIK_EINVAL;
+    const int rc = check_weights(N, K, 0, glu, experts ? experts : 1);
+    if (rc != QUIK_OK) return rc;
+    const quik::w4g::Layout l = quik::w4g::layout(N, K, 0, false, glu != 0, 1);
+    return quik::choose_w4g_form(rows, l.nt, l.kt, glu != 0, experts, experts && rows <= experts, cus);
+}
+
+int quik_debug_set_w4g_form(int form) {
+    if (form < -1 || form >= quik::kW4gForms) return QUIK_EINVAL;
+    quik::set_w4g_form(form);
+    return QUIK_OK;
+}
+
 int quik_moe_route(int type, const void* logits, int T, int experts, int ldl, const float* bias, int score, int groups,
                    int topk_groups, int group_top, int top_k, int renormalize, float scale, int32_t* ids, float* weights,
                    void* stream) {
@@ -123,6 +142,7 @@ int quik_moe_linear_w4g(int type, const void* x, int ldx, int x_per_slot, const 
     rc = check_product(type, x, T, K, ldx, w4, group, has_zero, glu, bias, N, experts, y, ldy);
     if (rc != QUIK_OK) return rc;
     if (x_per_slot != 0 && x_per_slot != 1) return QUIK_EINVAL;
+    if ((size_t)T * (x_per_slot ? top_k : 1) * ldx * 2 > kMaxOffset) return QUIK_EUNSUPPORTED;
     if (!ids || !workspace) return QUIK_ENULL;
     if (!aligned(ids, 4) || !aligned(weights, 4) || !aligned(workspace, 256)) return QUIK_EALIGN;
     const MoeWorkspace m = moe_workspace(T, top_k, glu ? N / 2 : N, experts, weights != nullptr);
