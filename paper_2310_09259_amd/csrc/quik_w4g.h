@@ -29,7 +29,8 @@ hipError_t launch_w4g(const W4gArgs& a, hipStream_t stream);
 // The kernels a product can run on: rows x channels of a workgroup's tile.  kW4gRows...: the waves split K (quik_w4g.hip);
 // kW4gTile...: quik_w4g_tiles.hip
 enum { kW4gRows16x16, kW4gRows16x32Wide, kW4gRows16x32, kW4gRows16x64, kW4gRows32x32, kW4gRows32x64,
-       kW4gTile32x128, kW4gTile64x128, kW4gTile128x128, kW4gTile256x128, kW4gTile256x256, kW4gForms };
+       kW4gTile32x128, kW4gTile64x128, kW4gTile128x128, kW4gTile256x128, kW4gTile256x256,
+       kW4gTile32x128Small, kW4gTile64x128Small, kW4gForms };    // (Small: several workgroups to a CU)
 // What the rules choose (host only; launch_w4g launches exactly this).  by_rows: a row at a time
 int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, int cus);
 void set_w4g_form(int form);                                            // test hook: -1 automatic

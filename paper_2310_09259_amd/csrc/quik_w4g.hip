@@ -77,9 +77,9 @@ __global__ __launch_bounds__(256) void pack_w4g_kernel(PackArgs a) {
 // Waves add up through LDS in wave order.
 //
 // MB, CB: row blocks and channel blocks of 16; NW waves.
-// Rows of a block: consecutive ones (dense), those of a block of the plan, or one (a row at a time).  TOKEN: with weights and
-// no plan a workgroup takes a token: the columns of its slots follow each other as if they were one long row, each slot's
-// scales multiplied by its weight.
+// Rows of a block: consecutive ones (dense), or one (experts: a row at a time).  TOKEN: with weights a workgroup takes a
+// token: the columns of its slots follow each other as if they were one long row, each slot's scales multiplied by its
+// weight.
 template <typename TY, int KG, int MB, int CB, int NW, int NST, bool TOKEN>
 // (the bound, of more threads than a launch has, keeps the compiler to 256 registers where LDS would allow it more)
 __global__ __launch_bounds__(512) void w4g_rows_kernel(W4gArgs a, int groups_n) {
@@ -97,57 +97,60 @@ __global__ __launch_bounds__(512) void w4g_rows_kernel(W4gArgs a, int groups_n) 
     const int b0 = id % groups_n * CB, block = id / groups_n;
 
     RowSource src{0, block * MB * 16, min(MB * 16, a.rows - block * MB * 16), false};
-    if (!TOKEN && a.plan) {
-        src = planned_rows(a.plan, a.experts, block, MB * 16);
-        if (src.count == 0) return;
-    } else if (TOKEN) {
+    if (TOKEN) {
         src = RowSource{0, block, 1, false};
     } else if (a.ids) {
         const int e = a.ids[block];
         src = RowSource{e >= 0 && e < a.experts ? e : -1, block, 1, false};
     }
-    const int32_t* const list = src.listed ? a.plan + a.experts + 2 + src.first : nullptr;
-
-    // ---- where this lane's copies come from.  x: by offsets from the first row (dense) or from x; copy i brings rows
+    // ---- where this lane's copies come from.  x: by offsets from the first row; copy i brings rows
     // 4 i .. 4 i + 3, its piece p of a row into place p ^ (row % 16), and zeros beyond the rows or beyond K
     const uint8_t* xbase = static_cast<const uint8_t*>(a.x);
     if (!a.ids) xbase += (size_t)src.first * a.ldx * 2;
-    else if (!list) xbase += (size_t)(TOKEN ? (a.x_per_slot ? block * a.top_k : block)
-                                            : (a.x_per_slot ? block : block / a.top_k)) * a.ldx * 2;
+    else xbase += (size_t)(TOKEN ? (a.x_per_slot ? block * a.top_k : block)
+                                 : (a.x_per_slot ? block : block / a.top_k)) * a.ldx * 2;
     const gemm_dev::v4i rx = whole_rsrc(xbase);
     uint32_t vo[X_COPIES];
 #pragma unroll
     for (int i = 0; i < X_COPIES; ++i) {
         const int r = 4 * i + g;
-        uint32_t row = list ? 0 : r;
-        if (list && r < src.count) row = (uint32_t)list[r] / (a.x_per_slot ? 1u : (uint32_t)a.top_k);
-        vo[i] = r < src.count ? row * (uint32_t)(a.ldx * 2) + ((l16 ^ (r & 15)) << 4) : kBeyond;
+        vo[i] = r < src.count ? (uint32_t)r * (uint32_t)(a.ldx * 2) + ((l16 ^ (r & 15)) << 4) : kBeyond;
     }
     // a block's scales in the first 128 bytes of its 256, its zero points (or zeros) in the second
     const size_t tile0 = (size_t)b0 * a.w.kt;
     const bool is_scale = lane < 8 * PER, is_zero = a.w.zeros && lane >= 32 && lane < 32 + 4 * PER;
     const uint32_t per_tile = is_zero ? kBlock * PER : kBlock * PER * 2;
 
+    // TOKEN: lane j has slot j's expert and weight (read from memory tile by tile, they would hold up every copy)
+    const int slot_r = block * a.top_k + min(lane, a.top_k - 1);
+    const int slot_e = TOKEN ? a.ids[slot_r] : 0;
+    const float slot_w = TOKEN ? a.weights[slot_r] : 0.0f;
+
     uint8_t* const ring = lds + wave * (NST * STAGE);
     const uint32_t ring_addr = gemm_dev::lds_addr(ring);
     const int tiles = src.expert < 0 ? 0 : TOKEN ? a.top_k * a.w.kt : a.w.kt;
     const int first = tiles * wave / NW, last = tiles * (wave + 1) / NW;
-    // tile vt of this wave's range, or past its end the last one again -> the weight of its slot
-    auto issue = [&](int vt, int slot) {
-        vt = min(vt, last - 1);
-        int kt = vt, e = src.expert, room = a.w.K;
+    // The next tile of this wave's range, or past its end the last one again -> the weight of its slot.  (next_kt, next_j: its
+    // columns and its slot; a division per tile would take longer than the tile)
+    int next = first, next_j = TOKEN && tiles > 0 ? first / a.w.kt : 0, next_kt = first - next_j * a.w.kt;
+    auto issue = [&](int slot) {
+        const int kt = next_kt;
+        int e = src.expert, room = a.w.K;
         uint32_t at = 0;
         float weight = 1.0f;
         if constexpr (TOKEN) {
-            const int j = vt / a.w.kt, r = block * a.top_k + j;
-            kt = vt - j * a.w.kt;
-            e = a.ids[r];
+            e = __builtin_amdgcn_readlane(slot_e, next_j);
             const bool on = e >= 0 && e < a.experts;
             e = on ? e : 0;
-            const float v = a.weights[r];
+            const float v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, slot_w), next_j));
             weight = on ? v : 0.0f;
             room = on ? room : 0;
-            at = (uint32_t)(a.x_per_slot ? j : 0) * (uint32_t)(a.ldx * 2);
+            at = (uint32_t)(a.x_per_slot ? next_j : 0) * (uint32_t)(a.ldx * 2);
+        }
+        if (next + 1 < last) {
+            ++next;
+            ++next_kt;
+            if (TOKEN && next_kt == a.w.kt) { next_kt = 0; ++next_j; }
         }
         room -= kt * kCols;
         at += (uint32_t)kt * 256;
@@ -229,17 +232,17 @@ __global__ __launch_bounds__(512) void w4g_rows_kernel(W4gArgs a, int groups_n) 
     if (first < last) {
         float ahead[NST - 1];                            // the weights of the tiles under way
 #pragma unroll
-        for (int d = 0; d < NST - 1; ++d) ahead[d] = issue(first + d, d);
+        for (int d = 0; d < NST - 1; ++d) ahead[d] = issue(d);
         int slot = 0, fill = NST - 1;
         for (int vt = first; vt < last; ++vt) {
             __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): the reads of the stage about to be filled are done
-            const float next = issue(vt + NST - 1, fill);
+            const float weight = issue(fill);
             gemm_dev::wait_vm<(NST - 1) * LPS>();        // tile vt has landed (this wave's own copies)
             asm volatile("" ::: "memory");
             multiply(ring + slot * STAGE, ahead[0]);
 #pragma unroll
             for (int d = 0; d < NST - 2; ++d) ahead[d] = ahead[d + 1];
-            ahead[NST - 2] = next;
+            ahead[NST - 2] = weight;
             slot = slot + 1 == NST ? 0 : slot + 1;
             fill = fill + 1 == NST ? 0 : fill + 1;
         }
@@ -284,7 +287,7 @@ __global__ __launch_bounds__(512) void w4g_rows_kernel(W4gArgs a, int groups_n) 
             const int i = m * 16 + 4 * g + r;
             if (i >= src.count) continue;
             const float y = src.expert < 0 ? 0.0f : a.glu ? silu_product(v[0][r], v[1][r]) : v[0][r];
-            const size_t row = list ? (size_t)list[i] : (size_t)src.first + i;
+            const size_t row = (size_t)src.first + i;
             if (a.weights && !TOKEN) a.stage[row * a.width + n] = y;
             else static_cast<uint16_t*>(a.y)[row * a.ldy + n] = TY::round(y);
         }
@@ -296,14 +299,13 @@ hipError_t launch_rows(const W4gArgs& a, hipStream_t stream) {
     const int groups_n = (a.w.nt + CB - 1) / CB;
     const dim3 threads(NW * 64);
     if constexpr (MB == 1) {
-        if (a.weights && !a.plan && !a.glu) {
+        if (a.weights && !a.glu) {
             hipLaunchKernelGGL((w4g_rows_kernel<TY, KG, 1, CB, NW, NST, true>), dim3((unsigned)(a.rows / a.top_k) * groups_n), threads, 0, stream, a, groups_n);
             return hipGetLastError();
         }
     }
     int blocks = (a.rows + MB * 16 - 1) / (MB * 16);
-    if (a.plan) blocks = a.rows / (MB * 16) + min(a.rows, a.experts + 1);
-    else if (a.ids) blocks = a.rows;
+    if (a.ids) blocks = a.rows;
     hipLaunchKernelGGL((w4g_rows_kernel<TY, KG, MB, CB, NW, NST, false>), dim3((unsigned)blocks * groups_n), threads, 0, stream, a, groups_n);
     return hipGetLastError();
 }
@@ -350,38 +352,41 @@ hipError_t launch_weight_pack_w4g(const void* w_q, int ldw, const void* w_scale,
 namespace { std::atomic<int> g_form{-1}; }
 void set_w4g_form(int form) { g_form.store(form, std::memory_order_relaxed); }
 
-// Up to 16 rows the choice goes by the channel blocks of all rows together (us, weights from HBM, K = 4096 unless noted):
+// Up to 16 rows, and for a row (or token) of experts at a time, the choice goes by the channel blocks of all of them together
+// (us, weights from HBM, K = 4096 unless noted):
 //  - one block per CU or fewer: single blocks and eight waves (N = 4096, 1 row: 6.0 against 6.7 with pairs, 7.4 with four
 //    waves); paired halves, and up to two per CU: pairs and eight waves;
 //  - more: pairs and four waves, two and three workgroups to a CU (N = 15360, K = 5120: 11.4 against 13.8 with eight waves);
 //    from six blocks per CU on four of them at a time (N = 28672, K = 8192: 24.9 against 26.9).
-// Above that the least of an estimate: rounds of workgroups, one to a CU, times the tiles of 128 columns that a wave (or
-// group of waves) goes through, times what such a step takes, plus a start.  Measured steps: 1.3 us and 1.75 for 32 x 32 and 32 x 64
-// (six waves split K), 0.95 and 1.3 for tiles of 32 x 128 and 64 x 128 (two groups split K), 1.2, 2.1 and 3.3 for
-// 128 x 128, 256 x 128 and 256 x 256.  N = 11008, chosen : best other one: 32 rows 13.5 : 17.3, 64 rows 17.9 : 23.6, 128 rows 23.3 : 33.7,
-// 256 rows 40 : 46, 512 rows 61 : 81, 1024 rows 102 : 128, 2048 rows 209 : 215; N = 4096, 256 rows 20.6 : 25;
-// N = 28672, K = 8192, 4096 rows 1630 : 1930.
-// Experts: the rows spread over all of them, each with half a tile to spare.
+// More rows of a dense layer: the least of an estimate, rounds of workgroups, one to a CU, times the tiles of 128 columns
+// that a wave (or group of waves) goes through, times what such a step takes, plus a start.  Measured steps: 1.3 us and 1.75
+// for 32 x 32 and 32 x 64 (six waves split K), 0.95 and 1.4 for tiles of 32 x 128 and 64 x 128 (two groups split K), 1.2,
+// 1.95 and 3.3 for 128 x 128, 256 x 128 and 256 x 256.  N = 11008, chosen : best other one: 24 rows 13.2 : 16.9, 48 rows
+// 19.8 : 22.3, 128 rows 23.3 : 31.9, 256 rows 39 : 42, 512 rows 60 : 69, 1024 rows 100 : 118, 2048 rows 199 : 214; N = 4096,
+// 1024 rows 45 : 47; N = 28672, K = 8192, 4096 rows 1550 : 1857.
+// Experts by a plan: workgroups of four waves, several to a CU, since each has few steps, and its start (its rows, its
+// first tiles) and its end would leave the CU idle.  Tiles of 32 rows up to about a hundred rows to an expert, then of 64:
+// 64 experts of 2048 x 2816 in halves, 28 rows each 94 : 109 (one workgroup to a CU: 132), 256 rows each 353 : 339 (390);
+// eight of 4096 x 4096, 16 rows each 39.5 : 45 (44), 128 rows each 89 : 87 (102), 512 rows each 242 : 217 (220).  Of fewer
+// than 2048 columns up to three hundred rows: 64 experts of 1408 x 2048, summed up, 256 rows each 226 : 249 (275).
 int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, int cus) {
-    const double active = experts ? min(rows, experts) : 0;
-    if (by_rows || (experts ? rows <= 4 * active : rows <= 16)) {
-        const double all = (double)blocks * (by_rows ? rows : experts ? active : 1);
+    if (by_rows || (!experts && rows <= 16)) {
+        const double all = (double)blocks * (by_rows ? rows : 1);
         if (all <= cus && !glu) return kW4gRows16x16;
         if (all <= 2 * cus) return kW4gRows16x32Wide;
         return all >= 6 * cus ? kW4gRows16x64 : kW4gRows16x32;
     }
+    if (experts) return rows <= (kt < 16 ? 300.0 : 100.0) * experts ? kW4gTile32x128Small : kW4gTile64x128Small;
     struct Cost { int form, rows, blocks, k_split; double start, step; };
     static const Cost costs[] = {
         {kW4gRows32x32, 32, 2, 6, 5.0, 1.3},     {kW4gRows32x64, 32, 4, 6, 5.0, 1.75},    {kW4gTile32x128, 32, 8, 2, 3.0, 0.95},
-        {kW4gTile64x128, 64, 8, 2, 3.0, 1.3},    {kW4gTile128x128, 128, 8, 1, 3.0, 1.2},  {kW4gTile256x128, 256, 8, 1, 3.0, 2.1},
+        {kW4gTile64x128, 64, 8, 2, 3.0, 1.4},    {kW4gTile128x128, 128, 8, 1, 3.0, 1.2},  {kW4gTile256x128, 256, 8, 1, 3.0, 1.95},
         {kW4gTile256x256, 256, 16, 1, 3.0, 3.3},
     };
     int best = kW4gTile256x256;
     double least = 1e30;
     for (const Cost& c : costs) {
-        double tiles = (rows + c.rows - 1) / c.rows;
-        if (experts) tiles = (double)rows / c.rows + active / 2 > active ? (double)rows / c.rows + active / 2 : active;
-        tiles *= (blocks + c.blocks - 1) / c.blocks;
+        const double tiles = (double)((rows + c.rows - 1) / c.rows) * ((blocks + c.blocks - 1) / c.blocks);
         const double t = c.start + ceil(tiles / cus) * ((kt + c.k_split - 1) / c.k_split) * c.step;
         if (t < least) { least = t; best = c.form; }
     }
@@ -391,18 +396,19 @@ int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by
 hipError_t launch_w4g(const W4gArgs& args, hipStream_t stream) {
     W4gArgs a = args;
     // a row (or a token and its slots) at a time where hardly two rows share an expert: no plan, no sums in memory
-    const bool by_rows = a.ids && a.rows <= a.experts;
+    const bool by_rows = a.ids && a.rows <= a.experts, by_token = by_rows && a.weights && !a.glu;
     if (by_rows) a.plan = nullptr;
     else if (a.ids) {
         if (hipError_t rc = launch_moe_plan(a.ids, a.rows, a.experts, a.plan, stream); rc != hipSuccess) return rc;
     }
     const int cus = compute_units();
     int form = g_form.load(std::memory_order_relaxed);
-    if (form < 0) form = choose_w4g_form(a.rows, a.w.nt, a.w.kt, a.glu, a.ids ? a.experts : 0, by_rows, cus > 0 ? cus : 256);
+    if (form < 0) form = choose_w4g_form(by_token ? a.rows / a.top_k : a.rows, a.w.nt, a.w.kt, a.glu, a.ids ? a.experts : 0, by_rows, cus > 0 ? cus : 256);
     if (by_rows && form > kW4gRows16x64) form = kW4gRows16x32;
+    if (a.ids && !by_rows && form < kW4gTile32x128) form = kW4gTile32x128Small;
     if (a.glu && form == kW4gRows16x16) form = kW4gRows16x32Wide;
     const hipError_t rc = form < kW4gTile32x128 ? launch_w4g_rows(a, form, stream) : launch_w4g_tiles(a, form, stream);
-    if (rc != hipSuccess || !a.weights || (by_rows && !a.glu)) return rc;
+    if (rc != hipSuccess || !a.weights || by_token) return rc;
     return launch_moe_combine(a.stage, a.ids, a.weights, a.rows / a.top_k, a.top_k, a.experts, a.width, a.bf16, a.y, a.ldy, stream);
 }
 

@@ -67,13 +67,15 @@ template <> struct ScaleOf<Bf16> { typedef Bf16Scale type; };
 
 // IB x JB blocks of 16 to a wave, WM x WN waves to a tile, KS groups of such waves that take every KS-th stage each and add
 // up through LDS at the end, in their order.  NST stages to a group: two where a stage is long enough to hide the next
-// one's way from memory (256 x 256: 2.9 us), three or four for the small tiles.
-template <typename TY, int KG, int IB, int JB, int WM, int WN, int KS, int NST>
-__global__ __launch_bounds__(512) void w4g_tiles_kernel(W4gArgs a, int tiles_m) {
+// one's way from memory (256 x 256: 2.9 us), three or four for the small tiles.  OCC waves per SIMD: two; four for the
+// smallest tile of experts, whose workgroups' starts and ends go on behind each other's products.
+template <typename TY, int KG, int IB, int JB, int WM, int WN, int KS, int NST, int OCC>
+__global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_tiles_kernel(W4gArgs a, int tiles_m) {
     constexpr int NW = WM * WN, BM = IB * WM * 16, BB = JB * WN, PER = kCols / KG;
     constexpr int COPIES = BM / 4 / NW;                  // of four rows each, per wave and stage
     static_assert(BM % (4 * NW) == 0 && BB % NW == 0 && JB % 2 == 0 && JB <= IB, "whole copies, whole pairs, at most a block widened per row block");
-    asm volatile("" ::: "v255");                         // the whole share of two waves per SIMD (see quik_gemm.hip)
+    if constexpr (OCC == 2) asm volatile("" ::: "v255"); // the whole share of the register file (see quik_gemm.hip)
+    else asm volatile("" ::: "v127");
     constexpr int W_COPIES = BB / NW;                    // of one weight tile each, per wave and stage
     // scales and zero points: with two stages straight into registers, a stage ahead; with more, where the wait for them must
     // not be one for later stages, through LDS, BPC blocks to a copy of 256 bytes
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(512) void w4g_tiles_kernel(W4gArgs a, int tiles_m) 
     v4f acc[IB][JB] = {};
     // row blocks of the next units: a unit of two matrix instructions is over before a read of LDS returns, so they are read
     // seven units ahead, or three where the registers are full; weights of this k-step and the next
-    constexpr int XR = IB * JB >= 32 ? 4 : 8, AHEAD = XR - 1;
+    constexpr int XR = IB * JB >= 32 || OCC > 2 ? 4 : 8, AHEAD = XR - 1;
     v4u x[XR], b[2][JB];
     uint32_t w[JB];                                      // packed weights of the next k-step
     const int row_at = (wm * IB * 16 + l16) * 256, w_at = X_BYTES + wn * JB * kTileBytes + lane * 16;
@@ -344,22 +346,24 @@ __global__ __launch_bounds__(512) void w4g_tiles_kernel(W4gArgs a, int tiles_m) 
     }
 }
 
-template <typename TY, int KG, int IB, int JB, int WM, int WN, int KS, int NST>
+template <typename TY, int KG, int IB, int JB, int WM, int WN, int KS, int NST, int OCC>
 hipError_t launch_tiles(const W4gArgs& a, hipStream_t stream) {
     const int bm = IB * WM * 16, tiles_m = a.ids ? a.rows / bm + min(a.rows, a.experts + 1) : (a.rows + bm - 1) / bm;
     const int tiles_n = (a.w.nt + JB * WN - 1) / (JB * WN);
-    hipLaunchKernelGGL((w4g_tiles_kernel<TY, KG, IB, JB, WM, WN, KS, NST>), dim3((unsigned)tiles_m * tiles_n), dim3(WM * WN * KS * 64), 0, stream, a, tiles_m);
+    hipLaunchKernelGGL((w4g_tiles_kernel<TY, KG, IB, JB, WM, WN, KS, NST, OCC>), dim3((unsigned)tiles_m * tiles_n), dim3(WM * WN * KS * 64), 0, stream, a, tiles_m);
     return hipGetLastError();
 }
 
 template <typename TY, int KG>
 hipError_t dispatch(const W4gArgs& a, int form, hipStream_t stream) {
     switch (form) {
-        case kW4gTile32x128: return launch_tiles<TY, KG, 2, 2, 1, 4, 2, 4>(a, stream);
-        case kW4gTile64x128: return launch_tiles<TY, KG, 4, 2, 1, 4, 2, 3>(a, stream);
-        case kW4gTile128x128: return launch_tiles<TY, KG, 4, 2, 2, 4, 1, 3>(a, stream);
-        case kW4gTile256x128: return launch_tiles<TY, KG, 8, 2, 2, 4, 1, 2>(a, stream);
-        case kW4gTile256x256: return launch_tiles<TY, KG, 8, 4, 2, 4, 1, 2>(a, stream);
+        case kW4gTile32x128: return launch_tiles<TY, KG, 2, 2, 1, 4, 2, 4, 2>(a, stream);
+        case kW4gTile64x128: return launch_tiles<TY, KG, 4, 2, 1, 4, 2, 3, 2>(a, stream);
+        case kW4gTile128x128: return launch_tiles<TY, KG, 4, 2, 2, 4, 1, 3, 2>(a, stream);
+        case kW4gTile256x128: return launch_tiles<TY, KG, 8, 2, 2, 4, 1, 2, 2>(a, stream);
+        case kW4gTile256x256: return launch_tiles<TY, KG, 8, 4, 2, 4, 1, 2, 2>(a, stream);
+        case kW4gTile32x128Small: return launch_tiles<TY, KG, 2, 2, 1, 4, 1, 2, 4>(a, stream);
+        case kW4gTile64x128Small: return launch_tiles<TY, KG, 4, 2, 1, 4, 1, 2, 2>(a, stream);
         default: return hipErrorInvalidValue;
     }
 }
