@@ -383,9 +383,10 @@ int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by
         {kW4gTile64x128, 64, 8, 2, 3.0, 1.4},    {kW4gTile128x128, 128, 8, 1, 3.0, 1.2},  {kW4gTile256x128, 256, 8, 1, 3.0, 1.95},
         {kW4gTile256x256, 256, 16, 1, 3.0, 3.3},
     };
-    int best = kW4gTile256x256;
+    int best = kW4gTile256x128;
     double least = 1e30;
     for (const Cost& c : costs) {
+        if (glu && c.form == kW4gTile256x256) continue;  // (see quik_w4g_tiles.hip)
         const double tiles = (double)((rows + c.rows - 1) / c.rows) * ((blocks + c.blocks - 1) / c.blocks);
         const double t = c.start + ceil(tiles / cus) * ((kt + c.k_split - 1) / c.k_split) * c.step;
         if (t < least) { least = t; best = c.form; }
@@ -407,6 +408,7 @@ hipError_t launch_w4g(const W4gArgs& args, hipStream_t stream) {
     if (by_rows && form > kW4gRows16x64) form = kW4gRows16x32;
     if (a.ids && !by_rows && form < kW4gTile32x128) form = kW4gTile32x128Small;
     if (a.glu && form == kW4gRows16x16) form = kW4gRows16x32Wide;
+    if (a.glu && form == kW4gTile256x256) form = kW4gTile256x128;
     const hipError_t rc = form < kW4gTile32x128 ? launch_w4g_rows(a, form, stream) : launch_w4g_tiles(a, form, stream);
     if (rc != hipSuccess || !a.weights || by_token) return rc;
     return launch_moe_combine(a.stage, a.ids, a.weights, a.rows / a.top_k, a.top_k, a.experts, a.width, a.bf16, a.y, a.ldy, stream);

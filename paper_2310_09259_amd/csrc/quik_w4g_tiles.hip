@@ -29,7 +29,7 @@ using gemm_dev::v4i;
 
 // The eight weights of one dword, scaled and rounded, in eight pieces of work (`part`, 0 .. 7) that stand between matrix
 // instructions.  fp16: (1024 + u) - (1032 + z) is exact, then one rounding
-struct HalfScale {
+template <bool FOLD> struct HalfScale {
     v2h scale, zero;
     __device__ __forceinline__ void set(uint32_t s, int z) {
         const _Float16 h = __builtin_bit_cast(_Float16, (uint16_t)s), c = (_Float16)(float)(1032 + z);
@@ -38,16 +38,17 @@ struct HalfScale {
     }
     __device__ __forceinline__ void widen(int part, uint32_t w, v4u& b, uint32_t mask, uint32_t bits) const {
         const int i = part >> 1;
+        if ((part & 1) && FOLD) return;
         if (part & 1) b[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, (uint32_t)b[i]) * scale);
         else b[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, ((w >> (4 * i)) & mask) | bits) - zero);
     }
 };
 // bf16: (1024 + u) s - (1032 + z) s is one fused multiply-add in fp32 whose result is exact (the scale has 11 bits), then
 // one rounding
-struct Bf16Scale {
+template <bool FOLD> struct Bf16Scale {
     float scale, zero;
     __device__ __forceinline__ void set(uint32_t s, int z) {
-        scale = (float)__builtin_bit_cast(_Float16, (uint16_t)s);
+        scale = FOLD ? 1.0f : (float)__builtin_bit_cast(_Float16, (uint16_t)s);
         zero = -(float)(1032 + z) * scale;
     }
     __device__ __forceinline__ void widen(int part, uint32_t w, v4u& b, uint32_t mask, uint32_t bits) const {
@@ -62,14 +63,14 @@ struct Bf16Scale {
         }
     }
 };
-template <typename TY> struct ScaleOf { typedef HalfScale type; };
-template <> struct ScaleOf<Bf16> { typedef Bf16Scale type; };
+template <typename TY, bool FOLD> struct ScaleOf { typedef HalfScale<FOLD> type; };
+template <bool FOLD> struct ScaleOf<Bf16, FOLD> { typedef Bf16Scale<FOLD> type; };
 
 // IB x JB blocks of 16 to a wave, WM x WN waves to a tile, KS groups of such waves that take every KS-th stage each and add
 // up through LDS at the end, in their order.  NST stages to a group: two where a stage is long enough to hide the next
 // one's way from memory (256 x 256: 2.9 us), three or four for the small tiles.  OCC waves per SIMD: two; four for the
 // smallest tile of experts, whose workgroups' starts and ends go on behind each other's products.
-template <typename TY, int KG, int IB, int JB, int WM, int WN, int KS, int NST, int OCC>
+template <typename TY, int KG, int IB, int JB, int WM, int WN, int KS, int NST, int OCC, bool FOLD>
 __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_tiles_kernel(W4gArgs a, int tiles_m) {
     constexpr int NW = WM * WN, BM = IB * WM * 16, BB = JB * WN, PER = kCols / KG;
     constexpr int COPIES = BM / 4 / NW;                  // of four rows each, per wave and stage
@@ -156,10 +157,17 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
     const uint32_t zero_mask = a.w.zeros ? 0xFFFFFFFFu : 0u;
     const uint32_t lane_group = l16 * PER;
     uint32_t sc[JB][(PER + 1) / 2], scn[JB][(PER + 1) / 2], ze[JB], zen[JB];
+    // FOLD: the scales of channels 4 g .. 4 g + 3, whose sums this lane has, [4][PER]; of the next stage; of the last group
+    uint32_t sf[JB][2 * PER] = {}, sfn[JB][2 * PER] = {};
+    _Float16 sl[JB][4] = {};
     auto fetch = [&](int kt, int j) {
         const size_t tile = (size_t)min(b0 + wn * JB + j, a.w.nt - 1) * a.w.kt + min(kt * KS + kg, a.w.kt - 1);
         const uint8_t* s = scales + tile * (kBlock * PER * 2) + lane_group * 2;
-        if constexpr (PER == 1) scn[j][0] = *reinterpret_cast<const uint16_t*>(s);
+        if constexpr (FOLD) {
+            const uint2* f = reinterpret_cast<const uint2*>(scales + tile * (kBlock * PER * 2) + (uint32_t)g * (8 * PER));
+#pragma unroll
+            for (int q = 0; q < PER; ++q) { const uint2 v = f[q]; sfn[j][2 * q] = v.x; sfn[j][2 * q + 1] = v.y; }
+        } else if constexpr (PER == 1) scn[j][0] = *reinterpret_cast<const uint16_t*>(s);
         else if constexpr (PER == 2) scn[j][0] = *reinterpret_cast<const uint32_t*>(s);
         else { const uint2 v = *reinterpret_cast<const uint2*>(s); scn[j][0] = v.x; scn[j][1] = v.y; }
         const uint8_t* z = zeros + tile * (kBlock * PER) + lane_group;
@@ -172,7 +180,8 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
         for (int j = 0; j < JB; ++j) {
             if constexpr (S_LDS) {
                 const uint8_t* const at = lds + slot + S_AT + (wn * JB + j) * (64 * PER);
-                if constexpr (PER == 1) sc[j][0] = *reinterpret_cast<const uint16_t*>(at + l16 * 2);
+                if constexpr (FOLD) ;
+                else if constexpr (PER == 1) sc[j][0] = *reinterpret_cast<const uint16_t*>(at + l16 * 2);
                 else if constexpr (PER == 2) sc[j][0] = *reinterpret_cast<const uint32_t*>(at + l16 * 4);
                 else { const uint2 v = *reinterpret_cast<const uint2*>(at + l16 * 8); sc[j][0] = v.x; sc[j][1] = v.y; }
                 if constexpr (PER == 1) ze[j] = at[32 + l16];
@@ -181,15 +190,43 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
                 continue;
             }
             ze[j] = zen[j] & zero_mask;
+            if constexpr (!FOLD) {
 #pragma unroll
-            for (int p = 0; p < (PER + 1) / 2; ++p) sc[j][p] = scn[j][p];
+                for (int p = 0; p < (PER + 1) / 2; ++p) sc[j][p] = scn[j][p];
+            }
+        }
+    };
+    // FOLD, at the start of a stage: its scales, and what the sums of the last group still need
+    auto take_fold = [&](uint32_t slot) {
+#pragma unroll
+        for (int j = 0; j < JB; ++j) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sl[j][r] = __builtin_bit_cast(_Float16, (uint16_t)(sf[j][(r * PER + PER - 1) / 2] >> (16 * ((r * PER + PER - 1) & 1))));
+            if constexpr (S_LDS) {
+                const uint2* f = reinterpret_cast<const uint2*>(lds + slot + S_AT + (wn * JB + j) * (64 * PER) + g * (8 * PER));
+#pragma unroll
+                for (int q = 0; q < PER; ++q) { const uint2 v = f[q]; sf[j][2 * q] = v.x; sf[j][2 * q + 1] = v.y; }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 2 * PER; ++q) sf[j][q] = sfn[j][q];
+            }
         }
     };
 
-    v4f acc[IB][JB] = {};
+    v4f acc[IB][JB] = {}, part[FOLD ? IB : 1][FOLD ? JB : 1] = {};
+    // FOLD: row block i's sums of group p of this stage, -1: of the stage before
+    auto fold = [&](int i, int p) {
+#pragma unroll
+        for (int j = 0; j < JB; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const _Float16 f = p < 0 ? sl[j][r] : __builtin_bit_cast(_Float16, (uint16_t)(sf[j][(r * PER + p) / 2] >> (16 * ((r * PER + p) & 1))));
+                acc[i][j][r] = __builtin_fmaf((float)f, part[FOLD ? i : 0][FOLD ? j : 0][r], acc[i][j][r]);
+            }
+    };
     // row blocks of the next units: a unit of two matrix instructions is over before a read of LDS returns, so they are read
     // seven units ahead, or three where the registers are full; weights of this k-step and the next
-    constexpr int XR = IB * JB >= 32 || OCC > 2 ? 4 : 8, AHEAD = XR - 1;
+    constexpr int XR = IB * JB * (FOLD ? 2 : 1) >= 32 || OCC > 2 ? 4 : 8, AHEAD = XR - 1;
     v4u x[XR], b[2][JB];
     uint32_t w[JB];                                      // packed weights of the next k-step
     const int row_at = (wm * IB * 16 + l16) * 256, w_at = X_BYTES + wn * JB * kTileBytes + lane * 16;
@@ -204,10 +241,10 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
     };
     uint32_t mask = 0x000F000Fu, bits = Half::kBits;     // (in registers: two literals would cost an instruction more)
     asm volatile("" : "+s"(mask), "+v"(bits));
-    typename ScaleOf<TY>::type s[JB];
+    typename ScaleOf<TY, FOLD>::type s[JB];
     auto scale = [&](int j, int ks) {
         const int p = ks * PER / 4;
-        s[j].set((sc[j][p / 2] >> (16 * (p & 1))) & 0xFFFFu, (int)(int8_t)(ze[j] >> (8 * p)));
+        s[j].set(FOLD ? 0u : (sc[j][p / 2] >> (16 * (p & 1))) & 0xFFFFu, (int)(int8_t)(ze[j] >> (8 * p)));
     };
     // A unit of work is one k-step of 32 columns and one row block: its JB matrix instructions and, between them, a share of
     // the widening of the next k-step's weights and the read of a row block some units ahead, so that LDS is read evenly.
@@ -217,9 +254,16 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
     auto unit = [&](int kt, int v) {
         const int ks = v / IB, i = v % IB, nks = (ks + 1) & 3;
         read(v + AHEAD);
+        if (FOLD && ks % (4 / PER) == 0) fold(i, ks * PER / 4 - 1);
 #pragma unroll
         for (int j = 0; j < JB; ++j) {
-            acc[i][j] = TY::mfma(b[ks & 1][j], x[v % XR], acc[i][j]);
+            if constexpr (FOLD) {
+                const v4f zero = {};
+                v4f& c = part[FOLD ? i : 0][FOLD ? j : 0];
+                c = TY::mfma(b[ks & 1][j], x[v % XR], ks % (4 / PER) == 0 ? zero : c);
+            } else {
+                acc[i][j] = TY::mfma(b[ks & 1][j], x[v % XR], acc[i][j]);
+            }
             const int third = v == FREE ? 0 : v + 1;
             if (third < 3) {
                 const int gap = third * JB + j;
@@ -263,6 +307,7 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
         }
     }
     for (int kt = 0; kt < kt_end; ++kt) {
+        if constexpr (FOLD) take_fold(cur);
 #pragma unroll
         for (int v = 0; v < READY; ++v) unit(kt, v);
         gemm_dev::wait_stage<(NST - 2) * ALL>();
@@ -282,6 +327,10 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
         nxt = nxt + STAGE == NST * STAGE ? 0 : nxt + STAGE;
     }
     gemm_dev::wait_vm<0>();                              // (the copies beyond the end)
+    if constexpr (FOLD) {
+#pragma unroll
+        for (int i = 0; i < IB; ++i) fold(i, PER - 1);
+    }
     if constexpr (KS > 1) {
         __syncthreads();
         float4* const red = reinterpret_cast<float4*>(all_lds);
@@ -346,24 +395,26 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
     }
 }
 
-template <typename TY, int KG, int IB, int JB, int WM, int WN, int KS, int NST, int OCC>
+template <typename TY, int KG, int IB, int JB, int WM, int WN, int KS, int NST, int OCC, bool FOLD>
 hipError_t launch_tiles(const W4gArgs& a, hipStream_t stream) {
     const int bm = IB * WM * 16, tiles_m = a.ids ? a.rows / bm + min(a.rows, a.experts + 1) : (a.rows + bm - 1) / bm;
     const int tiles_n = (a.w.nt + JB * WN - 1) / (JB * WN);
-    hipLaunchKernelGGL((w4g_tiles_kernel<TY, KG, IB, JB, WM, WN, KS, NST, OCC>), dim3((unsigned)tiles_m * tiles_n), dim3(WM * WN * KS * 64), 0, stream, a, tiles_m);
+    hipLaunchKernelGGL((w4g_tiles_kernel<TY, KG, IB, JB, WM, WN, KS, NST, OCC, FOLD>), dim3((unsigned)tiles_m * tiles_n), dim3(WM * WN * KS * 64), 0, stream, a, tiles_m);
     return hipGetLastError();
 }
 
 template <typename TY, int KG>
 hipError_t dispatch(const W4gArgs& a, int form, hipStream_t stream) {
     switch (form) {
-        case kW4gTile32x128: return launch_tiles<TY, KG, 2, 2, 1, 4, 2, 4, 2>(a, stream);
-        case kW4gTile64x128: return launch_tiles<TY, KG, 4, 2, 1, 4, 2, 3, 2>(a, stream);
-        case kW4gTile128x128: return launch_tiles<TY, KG, 4, 2, 2, 4, 1, 3, 2>(a, stream);
-        case kW4gTile256x128: return launch_tiles<TY, KG, 8, 2, 2, 4, 1, 2, 2>(a, stream);
-        case kW4gTile256x256: return launch_tiles<TY, KG, 8, 4, 2, 4, 1, 2, 2>(a, stream);
-        case kW4gTile32x128Small: return launch_tiles<TY, KG, 2, 2, 1, 4, 1, 2, 4>(a, stream);
-        case kW4gTile64x128Small: return launch_tiles<TY, KG, 4, 2, 1, 4, 1, 2, 2>(a, stream);
+        case kW4gTile32x128: return launch_tiles<TY, KG, 2, 2, 1, 4, 2, 4, 2, true>(a, stream);
+        case kW4gTile64x128: return launch_tiles<TY, KG, 4, 2, 1, 4, 2, 3, 2, true>(a, stream);
+        case kW4gTile128x128: return launch_tiles<TY, KG, 4, 2, 2, 4, 1, 3, 2, true>(a, stream);
+        case kW4gTile256x128:
+            if (a.glu) return launch_tiles<TY, KG, 8, 2, 2, 4, 1, 2, 2, true>(a, stream);
+            return launch_tiles<TY, KG, 8, 2, 2, 4, 1, 2, 2, false>(a, stream);
+        case kW4gTile256x256: return launch_tiles<TY, KG, 8, 4, 2, 4, 1, 2, 2, false>(a, stream);
+        case kW4gTile32x128Small: return launch_tiles<TY, KG, 2, 2, 1, 4, 1, 2, 4, true>(a, stream);
+        case kW4gTile64x128Small: return launch_tiles<TY, KG, 4, 2, 1, 4, 1, 2, 2, true>(a, stream);
         default: return hipErrorInvalidValue;
     }
 }
