@@ -947,7 +947,7 @@ def _matrix(t, dtypes, name, rows, cols, device):
         raise ValueError(f"{name} is on {t.device}, not on {device}")
     if cols > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must be contiguous along its last dimension")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), (cols + 7) // 8 * 8)   # (one row has no stride)
+    return t.stride(0) if t.shape[0] > 1 else (cols + 7) // 8 * 8         # (one row has no stride)
 
 
 def _whole(t, dtype, name, shape, device):

@@ -5,7 +5,7 @@ import math
 import numpy as np
 import pytest
 
-from tests.test_gpu_w4g import STEP, TINY, activations, bounds, check, layer, pack, silu_bounds
+from tests.test_gpu_w4g import ROUNDS, activations, bounds, check, forced, layer, pack, silu_bounds  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -131,7 +131,7 @@ def test_router_masks_that_leave_little_or_nothing(score, groups):
         assert bool(torch.isfinite(weights).all())
 
 
-def moe_reference(x, ids, W, wide, dtype, top_k, glu=False, bias=None, weights=None):
+def moe_reference(x, ids, W, wide, dtype, top_k, glu=False, bias=None, weights=None, rounds=False):
     """-> y, tolerance (float64), rows or weighted sums, of numpy inputs."""
     T = ids.shape[0]
     per_slot = x.shape[0] != T
@@ -140,7 +140,7 @@ def moe_reference(x, ids, W, wide, dtype, top_k, glu=False, bias=None, weights=N
     for r in range(T * top_k):
         e = ids.reshape(-1)[r]
         if 0 <= e < W.shape[0]:
-            a, t = bounds(x[None, r if per_slot else r // top_k], W[e], wide[e], dtype, None if bias is None else bias[e])
+            a, t = bounds(x[None, r if per_slot else r // top_k], W[e], wide[e], dtype, None if bias is None else bias[e], rounds)
             if glu:
                 a, t = silu_bounds(a, t)
             y[r], tol[r] = a[0], t[0]
@@ -229,3 +229,84 @@ def test_a_layer_of_experts_end_to_end_and_as_a_graph():
             torch.cuda.synchronize()
             for a, b in zip(captured, forward(x)):
                 assert torch.equal(a, b), (T, k)
+
+
+@pytest.mark.parametrize("form", range(13))
+@pytest.mark.parametrize("dtype,group,zero,glu,combine", [
+    ("float16", 128, True, False, True), ("bfloat16", 64, True, True, False), ("bfloat16", 32, False, False, True),
+    ("float16", 32, True, True, True)])
+@pytest.mark.parametrize("T,E,top_k", [(4, 16, 3), (90, 5, 2)])
+def test_every_kernel_on_every_kind_of_experts(forced, form, dtype, group, zero, glu, combine, T, E, top_k):
+    """A row (or token) at a time and by the plan, one expert with most of the rows."""
+    import torch
+    from paper_2310_09259_amd import api
+    K, N = 392, 146
+    raw = layer(form, N, K, group, zero, experts=E)
+    w = pack(raw, K, group, glu)
+    rng = np.random.Generator(np.random.PCG64(form))
+    ids = np.where(rng.random((T, top_k)) < 0.7, 2, rng.integers(-1, E + 1, (T, top_k))).astype(np.int32)
+    weights = rng.uniform(0.1, 1.0, (T, top_k)).astype(np.float32)
+    x = activations(form, T * top_k, K, dtype)
+    forced(form)
+    y = api.quik_moe_linear_w4g(x, torch.from_numpy(ids).cuda(), w, weights=torch.from_numpy(weights).cuda() if combine else None)
+    ref, tol = moe_reference(x.double().cpu().numpy(), ids, raw[3], raw[4], dtype, top_k, glu,
+                             weights=weights if combine else None, rounds=form in ROUNDS)
+    check(y, ref, tol, dtype)
+
+
+def test_nobody_is_chosen():
+    import torch
+    from paper_2310_09259_amd import api
+    w = pack(layer(1, 64, 128, 128, True, experts=4), 128, 128)
+    for T, top_k in ((1, 2), (40, 3)):
+        ids = torch.full((T, top_k), -1, dtype=torch.int32, device="cuda")
+        x = torch.full((T, 128), float("nan"), dtype=torch.float16, device="cuda")
+        weights = torch.full((T, top_k), float("nan"), device="cuda")
+        assert bool((api.quik_moe_linear_w4g(x, ids, w) == 0).all())
+        assert bool((api.quik_moe_linear_w4g(x, ids, w, weights=weights) == 0).all())
+
+
+def test_many_rows_of_one_expert_and_rows_past_the_plans_registers():
+    """More rows than the plan keeps between its passes, all but a few of one expert; every row's expert is right."""
+    import torch
+    from paper_2310_09259_amd import api
+    E, K, N, T, top_k = 6, 128, 32, 9001, 3
+    raw = layer(5, N, K, 128, False, experts=E)
+    w = pack(raw, K, 128)
+    rng = np.random.Generator(np.random.PCG64(3))
+    ids = np.where(rng.random((T, top_k)) < 0.9, 4, rng.integers(-1, E, (T, top_k))).astype(np.int32)
+    x = activations(7, T, K, "bfloat16")
+    y = api.quik_moe_linear_w4g(x, torch.from_numpy(ids).cuda(), w)
+    xs = x.double().cpu().numpy()
+    ref, tol = np.zeros((T * top_k, N)), np.zeros((T * top_k, N))
+    for e in range(E):
+        r = np.flatnonzero(ids.reshape(-1) == e)
+        ref[r], tol[r] = bounds(xs[r // top_k], raw[3][e], raw[4][e], "bfloat16")
+    check(y, ref, tol, "bfloat16")
+
+
+def test_refusals_of_the_binding():
+    import torch
+    from paper_2310_09259_amd import api
+    w = pack(layer(1, 64, 128, 128, True, experts=4), 128, 128)
+    dense = pack(layer(1, 64, 128, 128, True), 128, 128)
+    x = torch.zeros((3, 128), dtype=torch.float16, device="cuda")
+    ids = torch.zeros((3, 2), dtype=torch.int32, device="cuda")
+    weights = torch.zeros((3, 2), device="cuda")
+    small = torch.empty(16, dtype=torch.uint8, device="cuda")
+    for args, kw, err in (((x, ids, dense), {}, ValueError), ((x, ids.long(), w), {}, TypeError), ((x, ids[0], w), {}, TypeError),
+                          ((x, ids.t().contiguous().t(), w), {}, ValueError), ((x[:2], ids, w), {}, ValueError),
+                          ((x, ids, w), dict(weights=weights.half()), TypeError), ((x, ids, w), dict(weights=weights[:2]), ValueError),
+                          ((x, ids, w), dict(workspace=small), api.QuikError), ((x, ids.cpu(), w), {}, TypeError)):
+        with pytest.raises(err):
+            api.quik_moe_linear_w4g(*args, **kw)
+    with pytest.raises(ValueError):
+        api.quik_linear_w4g(x, w)
+    logits = torch.zeros((3, 8), device="cuda")
+    for kw, err in ((dict(top_k=9), api.QuikError), (dict(top_k=0), api.QuikError), (dict(top_k=2, groups=3), api.QuikError),
+                    (dict(top_k=2, bias=torch.zeros(8)), TypeError), (dict(top_k=2, bias=torch.zeros(7, device="cuda")), ValueError),
+                    (dict(top_k=2, score="tanh"), ValueError)):
+        with pytest.raises(err):
+            api.quik_moe_route(logits, **kw)
+    with pytest.raises(TypeError):
+        api.quik_moe_route(logits.double(), 2)

@@ -1,9 +1,9 @@
 """Layers with 4-bit weights in groups (quik_linear_w4g) against the definition in float64, through the C ABI.
 
 Tolerance, per output, with u = half a step of the output's type (fp16 2^-11, bf16 2^-8): the output is rounded once, u |y|;
-where the kernel rounds the weights to that type first, each product is off by u |x w| at most; the fp32 sums add 2^-24 of
-the absolute products per term, at most K terms deep (bf16 widens codes by an offset of 128, which makes products up to
-(136 + |q - z|) / |q - z| larger: its share is counted on 144 |x| s).  Nothing else is rounded."""
+where the kernel rounds the weights to that type first (ROUNDS), each product is off by u |x w| at most; the fp32 sums add
+2^-24 of the absolute products per term, at most K terms deep (bf16 widens codes by an offset of 128, which makes products up
+to (136 + |q - z|) / |q - z| larger: its share is counted on 144 |x| s).  Nothing else is rounded."""
 import numpy as np
 import pytest
 
@@ -11,6 +11,17 @@ pytestmark = pytest.mark.gpu
 
 STEP = {"float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
 TINY = {"float16": 2.0 ** -25, "bfloat16": 2.0 ** -134}      # half a step of the smallest numbers
+
+
+ROUNDS = (9, 10)                 # kernels (quik_debug_w4g_form) that may round the weights
+
+
+@pytest.fixture
+def forced():
+    """Sets the kernel of w4g products; automatic again afterwards."""
+    from paper_2310_09259_amd import api
+    yield api.quik_debug_set_w4g_form
+    api.quik_debug_set_w4g_form(-1)
 
 
 def layer(seed, N, K, group, zero, experts=0, pad=16):
@@ -45,14 +56,14 @@ def activations(seed, T, K, dtype, ld=None):
     return buf.cuda()[:, :K]
 
 
-def bounds(x, W, wide, dtype, bias=None):
+def bounds(x, W, wide, dtype, bias=None, rounds=False):
     """a (float64) and the tolerance of a before its final rounding; wide: |q - z| + 136 for every weight."""
     a = x @ W.T
     mag = np.abs(x) @ np.abs(W).T
     # |W| / |q - z| = the scale: sums of bf16 run on products of up to (|q - z| + 136) |x| s
     s = np.divide(np.abs(W), wide - 136.0, out=np.zeros_like(W), where=wide > 136.0)
     run = np.abs(x) @ (np.maximum(np.abs(W), s * wide) if dtype == "bfloat16" else np.abs(W)).T
-    tol = STEP[dtype] * mag + 2.0 ** -24 * (x.shape[1] + 8) * run
+    tol = (STEP[dtype] * mag if rounds else 0.0) + 2.0 ** -24 * (x.shape[1] + 8) * run
     if bias is not None:
         a = a + bias
         tol = tol + 2.0 ** -23 * np.abs(a)
@@ -104,7 +115,8 @@ def test_layer_against_its_definition(dtype, T, K, N, group, zero, glu, bias):
     x = activations(T + N, T, K, dtype, ld=K + 8 * (T % 3))
     b = torch.randn(N, generator=torch.Generator().manual_seed(5)).to(x.dtype).cuda() if bias else None
     y = api.quik_linear_w4g(x, w, bias=b)
-    a, tol = bounds(x.double().cpu().numpy(), raw[3], raw[4], dtype, None if b is None else b.double().cpu().numpy())
+    a, tol = bounds(x.double().cpu().numpy(), raw[3], raw[4], dtype, None if b is None else b.double().cpu().numpy(),
+                    rounds=api.quik_debug_w4g_form(T, N, K, glu) in ROUNDS)
     if glu:
         a, tol = silu_bounds(a, tol)
     check(y, a, tol, dtype)
@@ -150,3 +162,76 @@ def test_prepared_call_and_graph_replay_give_the_same_bits():
             torch.cuda.synchronize()
             assert torch.equal(z, api.quik_linear_w4g(x, w)), k
             assert torch.equal(z, first) == (k % 2 == 0)
+
+
+@pytest.mark.parametrize("form", range(13))
+@pytest.mark.parametrize("dtype,group,zero,glu,bias", [
+    ("float16", 128, True, False, True), ("bfloat16", 64, False, False, False), ("float16", 32, True, True, False),
+    ("bfloat16", 128, True, True, True), ("bfloat16", 32, True, False, False), ("float16", 64, False, True, True)])
+@pytest.mark.parametrize("T,K,N", [(3, 904, 146), (70, 392, 530), (275, 1288, 300)])
+def test_every_kernel_on_every_kind_of_layer(forced, form, dtype, group, zero, glu, bias, T, K, N):
+    """Odd numbers of tiles of columns, so that groups that split K end differently; ragged rows and channels."""
+    import torch
+    from paper_2310_09259_amd import api
+    raw = layer(form + T, N, K, group, zero)
+    w = pack(raw, K, group, glu)
+    x = activations(T + form, T, K, dtype)
+    b = torch.randn(N, generator=torch.Generator().manual_seed(6)).to(x.dtype).cuda() if bias else None
+    forced(form)
+    y = api.quik_linear_w4g(x, w, bias=b)
+    a, tol = bounds(x.double().cpu().numpy(), raw[3], raw[4], dtype, None if b is None else b.double().cpu().numpy(),
+                    rounds=form in ROUNDS)
+    if glu:
+        a, tol = silu_bounds(a, tol)
+    check(y, a, tol, dtype)
+
+
+def test_rows_far_into_a_matrix_of_more_than_4_gb(forced):
+    import torch
+    from paper_2310_09259_amd import api
+    T, ld, K, N = 70003, 32768, 256, 48                     # rows 64 KB apart: 4.6 GB
+    x = torch.empty((T, ld), dtype=torch.float16, device="cuda")[:, :K]
+    x.copy_(torch.randn((T, K), generator=torch.Generator().manual_seed(1)).half())
+    raw = layer(11, N, K, 128, True)
+    w = pack(raw, K, 128)
+    at = torch.tensor([0, 1, 40000, 65535, 65536, 65537, T - 2, T - 1])
+    a, tol = bounds(x[at.cuda()].double().cpu().numpy(), raw[3], raw[4], "float16", rounds=True)
+    for form in (-1, 5, 10):
+        forced(form)
+        check(api.quik_linear_w4g(x, w)[at.cuda()], a, tol, "float16")
+
+
+def test_other_stream_and_refusals_of_the_binding():
+    import torch
+    from paper_2310_09259_amd import api
+    raw = layer(2, 96, 256, 64, True)
+    w = pack(raw, 256, 64)
+    x = activations(1, 20, 256, "float16")
+    y = api.quik_linear_w4g(x, w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        z = api.quik_linear_w4g(x, w)
+        call, p = api.prepare_linear_w4g(x, w)
+    call()                                                  # on the stream it was prepared on
+    side.synchronize()
+    assert torch.equal(y, z) and torch.equal(y, p)
+    one = api.quik_linear_w4g(x[:1].t().contiguous().t(), w)   # one row, whatever its stride
+    assert torch.equal(one, y[:1])
+    for bad, err in ((x.float(), TypeError), (x[:, :248], ValueError), (x.t().contiguous().t(), ValueError), (x[0], ValueError),
+                     (x[:0], api.QuikError), (x[:1].expand(20, -1), api.QuikError), (x.cpu(), TypeError)):
+        with pytest.raises(err):
+            api.quik_linear_w4g(bad, w)
+    with pytest.raises(TypeError):
+        api.quik_linear_w4g(x, w, out=torch.empty((20, 96), dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(ValueError):
+        api.quik_linear_w4g(x, w, out=torch.empty((20, 95), dtype=torch.float16, device="cuda"))
+    with pytest.raises(ValueError):
+        api.quik_linear_w4g(x, w, bias=torch.zeros(95, dtype=torch.float16, device="cuda"))
+    with pytest.raises(ValueError):
+        api.quik_linear_w4g(x, w._replace(N=112))           # not what was packed
+    w_q, scale = torch.zeros((16, 64), dtype=torch.uint8, device="cuda"), torch.ones((16, 1), dtype=torch.float16, device="cuda")
+    for kw, err in ((dict(group=48), api.QuikError), (dict(group=64), ValueError), (dict(K=136, w_scale=scale.expand(16, 2).contiguous()), api.QuikError),
+                    (dict(w_scale=scale.float()), TypeError), (dict(w_zero=scale), TypeError), (dict(w_scale=None), TypeError)):
+        with pytest.raises(err):
+            api.quik_weight_pack_w4g(**{**dict(w_q=w_q, w_scale=scale, K=128, group=128), **kw})

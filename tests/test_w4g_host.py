@@ -64,7 +64,7 @@ PRODUCT_ERRORS = [
     (dict(y=ODD), EALIGN), (dict(bias=ODD), EALIGN)]
 
 
-@pytest.mark.parametrize("changes,rc", PRODUCT_ERRORS + [(dict(T=(1 << 24) + 1), EUNSUPPORTED)])
+@pytest.mark.parametrize("changes,rc", PRODUCT_ERRORS + [(dict(T=(1 << 24) + 1), EUNSUPPORTED), (dict(ldx=(1 << 22) + 8), EUNSUPPORTED)])
 def test_linear_refuses_bad_arguments(lib, changes, rc):
     assert lib.quik_linear_w4g(*_with(LINEAR, **changes)) == rc
 
@@ -73,7 +73,9 @@ def test_linear_refuses_bad_arguments(lib, changes, rc):
     (dict(top_k=0), EINVAL), (dict(top_k=33), EUNSUPPORTED), (dict(T=1 << 22, top_k=8), EUNSUPPORTED), (dict(experts=0), EINVAL),
     (dict(experts=1025), EUNSUPPORTED), (dict(x_per_slot=2), EINVAL), (dict(ids=NULL), ENULL), (dict(workspace=NULL), ENULL),
     (dict(ids=ODD), EALIGN), (dict(weights=ODD), EALIGN), (dict(workspace=P), EALIGN), (dict(workspace_bytes=16), EWORKSPACE),
-    (dict(weights=P, workspace_bytes=256), EWORKSPACE)])
+    (dict(weights=P, workspace_bytes=256), EWORKSPACE),
+    (dict(N=1 << 16, ldy=1 << 16, K=4096, ldx=4096, experts=1024), EUNSUPPORTED),      # 17 GB of scales
+    (dict(T=1 << 20, top_k=2, ldx=2048), EUNSUPPORTED), (dict(T=1 << 19, top_k=2, ldx=2048, x_per_slot=1), EUNSUPPORTED)])
 def test_experts_refuse_bad_arguments(lib, changes, rc):
     base = dict(type=0, x=P, ldx=128, x_per_slot=0, ids=P, weights=NULL, T=4, top_k=2, K=128, w4=P, group=32, has_zero=0,
                 glu=0, bias=NULL, N=16, experts=8, y=P, ldy=16, workspace=P256, workspace_bytes=1 << 20, stream=NULL)
@@ -113,3 +115,29 @@ def test_binding_refuses_what_it_cannot_pass_on():
         api.quik_moe_route(torch.zeros((2, 8)), 2)
     with pytest.raises(ValueError):
         api.quik_moe_route(torch.zeros((2, 8)), 2, score="relu")
+
+
+def test_kernel_choice(lib):
+    """Which kernel a product runs on, at the borders of the rules, and what is refused."""
+    form = lib.quik_debug_w4g_form
+    cus = 256
+    assert form(1, 4096, 4096, 0, 0, cus) == 0 and form(1, 4112, 4096, 0, 0, cus) == 1     # a block per CU, and one more
+    assert form(1, 4096, 4096, 1, 0, cus) == 1                                             # halves go in pairs
+    assert form(16, 8192, 4096, 0, 0, cus) == 1 and form(16, 8208, 4096, 0, 0, cus) == 2
+    assert form(16, 24560, 4096, 0, 0, cus) == 2 and form(16, 24576, 4096, 0, 0, cus) == 3
+    assert form(17, 4096, 4096, 0, 0, cus) == 4 and form(32, 11008, 4096, 0, 0, cus) == 5
+    assert form(48, 11008, 4096, 0, 0, cus) == 6 and form(128, 11008, 4096, 0, 0, cus) == 7
+    assert form(256, 11008, 4096, 0, 0, cus) == 8 and form(2048, 11008, 4096, 0, 0, cus) == 9
+    assert form(4096, 28672, 8192, 0, 0, cus) == 10 and form(4096, 28672, 8192, 1, 0, cus) != 10
+    assert form(64, 2816, 2048, 1, 64, cus) == 3 and form(65, 2816, 2048, 1, 64, cus) == 11    # a row at a time: up to one each
+    assert form(6400, 2816, 2048, 1, 64, cus) == 11 and form(6401, 2816, 2048, 1, 64, cus) == 12
+    assert form(19200, 2048, 1408, 0, 64, cus) == 11 and form(19201, 2048, 1408, 0, 64, cus) == 12
+    for rows in list(range(1, 70)) + [127, 129, 300, 1000, 5000, 1 << 20]:
+        for glu in (0, 1):
+            for experts in (0, 8, 1024):
+                assert 0 <= form(rows, 642, 904, glu, experts, cus) <= 12
+    for bad, rc in (((0, 64, 64, 0, 0, cus), EINVAL), ((1, 0, 64, 0, 0, cus), EINVAL), ((1, 64, 12, 0, 0, cus), EUNSUPPORTED),
+                    ((1, 63, 64, 1, 0, cus), EINVAL), ((1, 64, 64, 0, -1, cus), EINVAL), ((1, 64, 64, 0, 0, 0), EINVAL)):
+        assert form(*bad) == rc, bad
+    assert lib.quik_debug_set_w4g_form(13) == EINVAL and lib.quik_debug_set_w4g_form(-2) == EINVAL
+    assert lib.quik_debug_set_w4g_form(3) == OK and lib.quik_debug_set_w4g_form(-1) == OK
