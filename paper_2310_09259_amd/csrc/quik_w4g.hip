@@ -365,10 +365,10 @@ void set_w4g_form(int form) { g_form.store(form, std::memory_order_relaxed); }
 // 19.8 : 22.3, 128 rows 23.3 : 31.9, 256 rows 39 : 42, 512 rows 60 : 69, 1024 rows 100 : 118, 2048 rows 199 : 214; N = 4096,
 // 1024 rows 45 : 47; N = 28672, K = 8192, 4096 rows 1550 : 1857.
 // Experts by a plan: workgroups of four waves, several to a CU, since each has few steps, and its start (its rows, its
-// first tiles) and its end would leave the CU idle.  Tiles of 32 rows up to about a hundred rows to an expert, then of 64:
-// 64 experts of 2048 x 2816 in halves, 28 rows each 94 : 109 (one workgroup to a CU: 132), 256 rows each 353 : 339 (390);
-// eight of 4096 x 4096, 16 rows each 39.5 : 45 (44), 128 rows each 89 : 87 (102), 512 rows each 242 : 217 (220).  Of fewer
-// than 2048 columns up to three hundred rows: 64 experts of 1408 x 2048, summed up, 256 rows each 226 : 249 (275).
+// first tiles) and its end would leave the CU idle.  Tiles of 32 rows up to about a hundred rows to an expert, then of 64 (in
+// brackets the best with one workgroup to a CU): 64 experts of 2048 x 2816 in halves, bf16, groups of 64, 28 rows each 116 : 130 (158);
+// fp16, 256 rows each 337 : 293 (409); of 1408 x 2048, summed up, 256 rows each 231 : 213 (281); eight of 4096 x 4096 in
+// halves, 16 rows each 39.4 : 44 (42), 128 rows each 83 : 84 (101), 512 rows each 226 : 194 (252).
 int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, int cus) {
     if (by_rows || (!experts && rows <= 16)) {
         const double all = (double)blocks * (by_rows ? rows : 1);
@@ -376,7 +376,7 @@ int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by
         if (all <= 2 * cus) return kW4gRows16x32Wide;
         return all >= 6 * cus ? kW4gRows16x64 : kW4gRows16x32;
     }
-    if (experts) return rows <= (kt < 16 ? 300.0 : 100.0) * experts ? kW4gTile32x128Small : kW4gTile64x128Small;
+    if (experts) return rows <= 100.0 * experts ? kW4gTile32x128Small : kW4gTile64x128Small;
     struct Cost { int form, rows, blocks, k_split; double start, step; };
     static const Cost costs[] = {
         {kW4gRows32x32, 32, 2, 6, 5.0, 1.3},     {kW4gRows32x64, 32, 4, 6, 5.0, 1.75},    {kW4gTile32x128, 32, 8, 2, 3.0, 0.95},

@@ -1,14 +1,19 @@
 // Products with 4-bit weights in groups for many rows (quik_w4g.hip has the few): tiles of the output on the 16-bit
 // matrix instructions.
 //
-// What bounds it: the matrix pipes, and beside them the vector instructions that widen the weights.  A wave of IB x JB
-// blocks of 16 x 16 outputs takes its weights from memory straight into registers, in the lane order that the layout gives
-// them (16 bytes of a lane are four instructions' worth), and widens them for all its IB row blocks: fp16 in 15 vector
-// instructions per eight weights, bf16 in 23, against 8 * IB matrix instructions of 16 clocks per four of those.  128 rows
-// to a wave keep that at half the matrix time in fp16; fewer rows cannot.  Widened weights in LDS, once per workgroup,
-// would be read back at 1.5 times the bytes that the activations already take of it.
-// The weights are rounded to the type of x, s (q - z), once each: a scale applied to fp32 partial sums of a group would
-// need a second set of accumulators, or one more fused multiply-add per output and group on vector pipes that are full.
+// What bounds it: the matrix pipes and, in turn rather than at the same time (a step's clocks come close to the sum of both), the
+// vector instructions that widen the weights.  A wave of IB x JB blocks of 16 x 16 outputs reads its weights from LDS in the
+// lane order that the layout gives them and widens them for all its IB row blocks: eight weights take 11 to 19 vector
+// instructions of 4 clocks, against IB / 4 matrix instructions of 16.  128 rows to a wave keep that at a third to a half of the
+// matrix time; fewer rows cannot.  Widened weights in LDS, once per workgroup, would be read back at 1.5 times the bytes
+// that the activations already take of it.
+//
+// FOLD: the widened weights are the integers q - z, exact in either type, a group's sums of products have registers of their
+// own, and the scale is applied to these fp32 sums, one fused multiply-add per output and group.  The two largest tiles
+// have no room for that (256 x 256), or it costs them up to a half of their time in groups of 32 (256 x 128: 319 us against
+// 210 for 2048 x 4096 x 11008, 8 % in groups of 128): there the weights are rounded to the type of x, s (q - z), once each.  In paired
+// halves, whose product shows both factors' errors, that made 1.7 times the output's own rounding: 256 x 128 folds, and 256 x 256
+// does not run.
 //
 // The activations of 128 columns go through LDS, two stages, copied without passing through registers; rows are 256
 // bytes, their sixteen 16-byte pieces exchanged by the row's number so that sixteen rows' pieces of one k fall into
@@ -75,7 +80,9 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
     constexpr int NW = WM * WN, BM = IB * WM * 16, BB = JB * WN, PER = kCols / KG;
     constexpr int COPIES = BM / 4 / NW;                  // of four rows each, per wave and stage
     static_assert(BM % (4 * NW) == 0 && BB % NW == 0 && JB % 2 == 0 && JB <= IB, "whole copies, whole pairs, at most a block widened per row block");
-    if constexpr (OCC == 2) asm volatile("" ::: "v255"); // the whole share of the register file (see quik_gemm.hip)
+    // the whole share of the register file (see quik_gemm.hip); of the 168 registers of three waves all but the last
+    if constexpr (OCC == 2) asm volatile("" ::: "v255");
+    else if constexpr (OCC == 3) asm volatile("" ::: "v166");
     else asm volatile("" ::: "v127");
     constexpr int W_COPIES = BB / NW;                    // of one weight tile each, per wave and stage
     // scales and zero points: with two stages straight into registers, a stage ahead; with more, where the wait for them must
@@ -414,7 +421,7 @@ hipError_t dispatch(const W4gArgs& a, int form, hipStream_t stream) {
             return launch_tiles<TY, KG, 8, 2, 2, 4, 1, 2, 2, false>(a, stream);
         case kW4gTile256x256: return launch_tiles<TY, KG, 8, 4, 2, 4, 1, 2, 2, false>(a, stream);
         case kW4gTile32x128Small: return launch_tiles<TY, KG, 2, 2, 1, 4, 1, 2, 4, true>(a, stream);
-        case kW4gTile64x128Small: return launch_tiles<TY, KG, 4, 2, 1, 4, 1, 2, 2, true>(a, stream);
+        case kW4gTile64x128Small: return launch_tiles<TY, KG, 4, 2, 1, 4, 1, 2, KG == 128 ? 3 : 2, true>(a, stream);
         default: return hipErrorInvalidValue;
     }
 }
