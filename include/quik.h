@@ -483,8 +483,8 @@ int quik_linear_sp24(const void *x, int T, int K, int ldx, const int32_t *outlie
  *   y[t, n] = a[t, n]                                          (glu = 0; y has N columns)
  *   y[t, f] = a[t, f] * sigmoid(a[t, f]) * a[t, N / 2 + f]     (glu = 1; N even, y has N / 2 columns: the first half of the
  *                                                              channels are gates, the second half values)
- * Sums are fp32 and y is rounded once.  For few rows the scale is applied to fp32 sums of exact products;
- * kernels for more (quik_debug_w4g_form 6 and up) first round the weights to the type of x, once per weight.
+ * Sums are fp32 and y is rounded once.  The scale is applied to fp32 sums of exact products, but for the largest
+ * tiles of a plain layer (quik_debug_w4g_form 9 and 10): they first round the weights to the type of x, once per weight.
  * A row of x with an infinity or a NaN gives a row of y without meaning; other rows are not affected.
  *
  *  quik_weight_pack_w4g   once per layer: codes, scales and zero points -> w4 (quik_w4g_bytes(...) bytes, 16-byte aligned).

@@ -17,14 +17,6 @@ __device__ __forceinline__ gemm_dev::v4i whole_rsrc(const void* p) {
     return r;
 }
 
-__device__ __forceinline__ gemm_dev::v4i buffer_load16(gemm_dev::v4i rsrc, uint32_t voff, uint32_t soff) {
-    typedef unsigned u4 __attribute__((ext_vector_type(4)));
-    const u4 r = __builtin_bit_cast(u4, rsrc);
-    const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(
-        reinterpret_cast<void*>((uint64_t)r[0] | (uint64_t)r[1] << 32), (short)0, (int)r[2], (int)r[3]);
-    return __builtin_bit_cast(gemm_dev::v4i, __builtin_amdgcn_raw_buffer_load_b128(d, (int)voff, (int)soff, 0));
-}
-
 struct RowSource {
     int expert;                      // -1: none, the rows are zeros
     int first, count;                // rows first .. first + count - 1 of the list, or of the output
@@ -32,7 +24,7 @@ struct RowSource {
 };
 
 // The rows of block b of a plan, bm to a block: the blocks of an expert's rows follow each other, then those of no expert;
-// count 0 beyond the last.  A lane of each wave looks at four experts; every wave finds the same.  (At most 1024 experts.)
+// count 0 beyond the last.  Every wave finds the same, 64 experts at a time, one to a lane.  (At most 1024 experts.)
 __device__ __forceinline__ RowSource planned_rows(const int32_t* plan, int experts, int b, int bm) {
     const int lane = threadIdx.x & 63;
     RowSource r{-1, 0, 0, true};
