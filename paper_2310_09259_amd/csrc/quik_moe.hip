@@ -21,7 +21,7 @@ using namespace w4g;
 // chosen ones, the first not chosen, or groups next to the border lie within the error of the fp32 scores of each other goes
 // through the same in float64 (of random logits one token in some thousands).  Four groups of experts are reduced side by
 // side.  4096 tokens and 256 experts in eight groups: 33 us all in float64, with shuffles through LDS; 24.9 one group after
-// another; 20.7 to 24.0 as it is, by the tokens that go through float64 (for one token 10.4 and 9.2).
+// another; 20.7 to 24.0 as it is, by the tokens that go through float64 (for one token 10.4 and 9.5).
 
 template <int CTRL, int ROWS> __device__ __forceinline__ float lane_move(float v) {
     const int i = __builtin_bit_cast(int, v);
@@ -172,6 +172,7 @@ __device__ __forceinline__ bool route_token(const MoeRouteArgs& a, int t, const 
                 if (SIDE == 1 && v[0] == kOut) break;         // (nothing is left in it)
 #pragma unroll
                 for (int q = 0; q < SIDE; ++q) {
+                    if (v[q] < 0 && v[q] > kOut) sure = false;                 // (a sum may be small beside what it is made of)
                     sum[q] = k && v[q] > kOut ? sum[q] + v[q] : k ? sum[q] : v[q];
                     const int from = __ffsll(__ballot(best[q] == v[q])) - 1;   // (one of equal ones: the sum is the same)
 #pragma unroll

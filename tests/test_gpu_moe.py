@@ -105,6 +105,17 @@ def test_router_choices_next_to_a_border(score):
         assert np.array_equal(ids.cpu().numpy(), ref)
 
 
+def test_groups_whose_sums_are_small_differences_of_large_choices():
+    """Biases of 2^20 and -2^20 in every group: in fp32 the choices are multiples of 2^-3 and 2^-4, and the sums, 1.04 and 1.08,
+    come out the other way round."""
+    import torch
+    scores = [[0.57, 0.47, 0.2, 0.2], [0.55, 0.53, 0.2, 0.2]]
+    logits = torch.tensor([math.log(p / (1 - p)) for g in scores for p in g], dtype=torch.float32).reshape(1, 8).cuda()
+    bias = np.array([2.0 ** 20, -2.0 ** 20, -2.0 ** 21, -2.0 ** 21] * 2, np.float32)
+    ids, _ = check_route(logits, top_k=2, bias=bias, score="sigmoid", groups=2, topk_groups=1, group_top=2)
+    assert ids.tolist() == [[4, 5]]
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("groups", [1, 4])
 def test_router_masks_that_leave_little_or_nothing(score, groups):
