@@ -485,7 +485,8 @@ int quik_linear_sp24(const void *x, int T, int K, int ldx, const int32_t *outlie
  *                                                              channels are gates, the second half values)
  * Sums are fp32 and y is rounded once.  The scale is applied to fp32 sums of exact products, but for the largest
  * tiles of a plain layer (quik_debug_w4g_form 9 and 10): they first round the weights to the type of x, once per weight.
- * A row of x with an infinity or a NaN gives a row of y without meaning; other rows are not affected.
+ * A row of x with an infinity, a NaN or (bf16) a value from 2^112 on, whose sums over a group fp32 may not hold, gives a
+ * row of y without meaning; other rows are not affected.
  *
  *  quik_weight_pack_w4g   once per layer: codes, scales and zero points -> w4 (quik_w4g_bytes(...) bytes, 16-byte aligned).
  *    w_q       packed signed 4-bit codes [N, ldw bytes] in the weight nibble order of this header, ldw >= K / 2
