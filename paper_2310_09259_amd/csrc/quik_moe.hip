@@ -96,13 +96,17 @@ __device__ __forceinline__ bool route_token(const MoeRouteArgs& a, int t, const 
         for (int i = 0; i < VPL; ++i) score[i] = (F)1 / ((F)1 + exp(-(F)logit[i]));
     } else {
         top = wave_max(top);
-        F total = 0;
+        F part[VPL];
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
             score[i] = logit[i] == -INFINITY ? (F)0 : logit[i] == top ? (F)1 : exp((F)logit[i] - (F)top);
-            total += score[i];
+            part[i] = score[i];
         }
-        total = wave_sum(total);
+#pragma unroll
+        for (int d = 1; d < VPL; d *= 2)                 // (in pairs: four roundings of sixteen scores)
+#pragma unroll
+            for (int i = 0; i + d < VPL; i += 2 * d) part[i] += part[i + d];
+        const F total = wave_sum(part[0]);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) score[i] /= total; // (nobody: NaN, and not looked at)
         largest = (F)1 / total;
@@ -112,9 +116,12 @@ __device__ __forceinline__ bool route_token(const MoeRouteArgs& a, int t, const 
         const F c = score[i] + (F)bias[i];
         choice[i] = logit[i] == -INFINITY || c != c ? kOut : c;
     }
-    // A score is off by 2^-21 of itself and of the largest (the exponential is good to two units, its argument to a half, the
-    // sum of 1024 and the quotient add four), its choice by one rounding more; two of them by twice that.
-    const F apart = (F)0x1p-19 * largest;
+    // How far apart two fp32 choices have to lie, in units of 2^-24.  The exponential is off by 4 of itself.  Sigmoid: times
+    // 1 - s, and a unit each for the sum and the quotient, 6 s - 4 s^2 < 2.3 for a score, 4.6 for two.  Softmax, of the largest
+    // score: 4.4 with the argument's rounding and one for the quotient, 10.8 for two, and what all have in common (it matters
+    // beside a bias), 4.4 and ten roundings of the total: 25.2.  The choices' own rounding, and that of sums of such that are
+    // not negative: one of each, or of every term, of the two.
+    const F apart = a.sigmoid ? (F)0x1p-21 : (F)0x1p-19 * largest, rounding = (F)0x1p-22;
     bool sure = true;
     // the largest choice, its expert e (of equal ones the lowest), taken out of the list, its score, logit and bias;
     // -infinity: there is none
@@ -190,7 +197,7 @@ __device__ __forceinline__ bool route_token(const MoeRouteArgs& a, int t, const 
             const F v = wave_max(mine);
             if (v == kOut) break;
             if (k == a.topk_groups) {                    // the first group that goes
-                sure = sure && last - v > a.group_top * (apart + (F)0x1p-21 * fabs(last));
+                sure = sure && last - v > a.group_top * (apart + rounding * fabs(last));
                 break;
             }
             const int at = __ffsll(__ballot(mine == v)) - 1;
@@ -214,7 +221,7 @@ __device__ __forceinline__ bool route_token(const MoeRouteArgs& a, int t, const 
         const F v = pick(e, s, l, b);
         if (v == kOut) break;
         // equal for certain (the index decides), or apart for certain
-        if (j > 0) sure = sure && ((l == last_l && b == last_b) || last - v > apart + (F)0x1p-21 * fabs(last));
+        if (j > 0) sure = sure && ((l == last_l && b == last_b) || last - v > apart + rounding * fabs(last));
         if ((!EXACT && !sure) || j == a.top_k) break;
         last = v;
         last_l = l;
