@@ -232,12 +232,13 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
             }
     };
     // row blocks of the next units: a unit of two matrix instructions is over before a read of LDS returns, so they are read
-    // seven units ahead, or three where the registers are full; weights of this k-step and the next
-    constexpr int XR = IB * JB * (FOLD ? 2 : 1) >= 32 || OCC > 2 ? 4 : 8, AHEAD = XR - 1;
+    // seven units ahead, or three where the registers are full; weights of this k-step and the next.  (Not so far that the
+    // next stage's are read before this stage's copies have all been issued, in its first two units: see READY)
+    constexpr int UNITS = 4 * IB, COPIED = 2;
+    constexpr int XR = IB * JB * (FOLD ? 2 : 1) >= 32 || OCC > 2 ? 4 : 8, AHEAD = XR - 1 < UNITS - COPIED ? XR - 1 : UNITS - COPIED;
     v4u x[XR], b[2][JB];
     uint32_t w[JB];                                      // packed weights of the next k-step
     const int row_at = (wm * IB * 16 + l16) * 256, w_at = X_BYTES + wn * JB * kTileBytes + lane * 16;
-    constexpr int UNITS = 4 * IB;
     uint32_t cur = 0, nxt = STAGE, prv = (NST - 1) * STAGE;   // the ring's bytes of this, the next and the last stage
     auto read = [&](int v) {                             // activations of unit v, which may be one of the next stage's
         const int i = v % IB, ks = v / IB & 3;
@@ -257,7 +258,10 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
     // the widening of the next k-step's weights and the read of a row block some units ahead, so that LDS is read evenly.
     // Before the unit READY a barrier says that the next stage is there, before the last unit of all another that this one is
     // read and may be filled; the copies follow in the gaps of three units.
+    // The wait at READY leaves the copies of the NST - 2 stages behind the next one under way, and counts on the last of these
+    // being issued by then.
     constexpr int READY = 3 * IB - 1 < UNITS - AHEAD ? 3 * IB - 1 : UNITS - AHEAD, FREE = UNITS - 1, ALL = COPIES + W_COPIES + S_COPIES, PIECES = 8 * JB / IB;
+    static_assert(READY >= COPIED && READY <= UNITS - AHEAD && UNITS % XR == 0, "the wait counts whole stages; no read in front of it");
     auto unit = [&](int kt, int v) {
         const int ks = v / IB, i = v % IB, nks = (ks + 1) & 3;
         read(v + AHEAD);
@@ -271,7 +275,7 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
             } else {
                 acc[i][j] = TY::mfma(b[ks & 1][j], x[v % XR], acc[i][j]);
             }
-            const int third = v == FREE ? 0 : v + 1;
+            const int third = v == FREE ? 0 : v + 1;     // (the last one in unit COPIED - 1)
             if (third < 3) {
                 const int gap = third * JB + j;
 #pragma unroll
