@@ -18,8 +18,8 @@ using namespace w4g;
 // What bounds it: the chain of reductions over the wave, some ten of them one behind the other, and for one token the
 // latency of its logits; the bytes are nothing.  So maxima and sums go through the lanes' data paths (six vector
 // instructions, no trip to LDS), and scores are computed in fp32.  Choices are told apart as float64 tells them: a token whose
-// chosen ones, the first not chosen, or groups next to the border lie within the error of the fp32 scores of each other goes
-// through the same in float64 (of random logits one token in some thousands).  Four groups of experts are reduced side by
+// chosen ones, the first not chosen, or groups next to the border lie within the error of the fp32 scores of each other, or
+// one of whose chosen scores is below 2^-100, goes through the same in float64.  Four groups of experts are reduced side by
 // side.  4096 tokens and 256 experts in eight groups: 33 us all in float64, with shuffles through LDS; 24.9 one group after
 // another; 20.7 to 24.0 as it is, by the tokens that go through float64 (for one token 10.4 and 9.5).
 
@@ -76,7 +76,7 @@ __device__ __forceinline__ float load_logit(const void* p, int type, size_t at) 
 }
 
 // A token, with scores in F; logit: -infinity for an expert that takes no part.  float: false, with nothing written, if it may
-// have told choices apart otherwise than double.
+// have told choices apart otherwise than double, or a chosen score is next to what fp32 cannot hold.
 template <typename F, int VPL>
 __device__ __forceinline__ bool route_token(const MoeRouteArgs& a, int t, const float (&logit)[VPL]) {
     constexpr bool EXACT = sizeof(F) == 8;
@@ -220,6 +220,8 @@ __device__ __forceinline__ bool route_token(const MoeRouteArgs& a, int t, const 
         float l = 0.0f, b = 0.0f;
         const F v = pick(e, s, l, b);
         if (v == kOut) break;
+        // a score that fp32 still holds all bits of, and weights are made of (in a sum of smaller ones they would vanish)
+        if (!EXACT && j < a.top_k) sure = sure && s >= (F)0x1p-100;
         // equal for certain (the index decides), or apart for certain
         if (j > 0) sure = sure && ((l == last_l && b == last_b) || last - v > apart + rounding * fabs(last));
         if ((!EXACT && !sure) || j == a.top_k) break;

@@ -1,0 +1,66 @@
+"""The router's weights where a softmax or sigmoid in fp32 has nothing left of the chosen experts' scores: against the
+definition in float64.  Tolerance as in test_gpu_moe: such tokens' scores are computed in float64 and their weights rounded to
+fp32 once, the others' are good to 2^-18."""
+import math
+
+import numpy as np
+import pytest
+
+from tests.test_gpu_moe import check_route
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+
+
+def _logits(rows):
+    import torch
+    return torch.tensor(rows, dtype=torch.float32).cuda()
+
+
+@pytest.mark.parametrize("groups", [1, 4])
+@pytest.mark.parametrize("logit", [-20.0, -60.0, -69.0, -70.0, -88.0, -89.0, -90.0, -100.0, -104.0, -300.0, -740.0])
+def test_lone_experts_far_below_keep_their_weight(logit, groups):
+    """Everything else is masked: one expert has all the weight, two equal ones half each.  (Below -709 there is nothing to
+    divide: e^740 > 2^1024, so that the sigmoid is 0 in float64, and the weights of a sum of 0 are 0.)"""
+    rows = np.full((3, 8), -INF, np.float32)
+    rows[0, 3] = logit
+    rows[1, [1, 6]] = logit
+    rows[2, [0, 7]] = logit, logit - 1.0
+    ids, w = check_route(_logits(rows), top_k=2, score="sigmoid", groups=groups, topk_groups=min(groups, 2), group_top=1)
+    assert ids.tolist()[:2] == [[3, -1], [1, 6]]
+    assert w.tolist()[:2] == ([[1.0, 0.0], [0.5, 0.5]] if logit > -709 else [[0.0, 0.0]] * 2)
+
+
+def test_a_bias_chooses_experts_whose_softmax_is_nothing_beside_the_largest():
+    rows = _logits([[0.0, -120.0, -120.0], [0.0, -120.0, -121.0], [0.0, -88.0, -90.0], [0.0, -100.0, -103.0]])
+    bias = np.array([-2.0, 0.0, 0.0], np.float32)
+    ids, w = check_route(rows, top_k=2, bias=bias, score="softmax")
+    assert ids.tolist() == [[1, 2]] * 4 and w[0].tolist() == [0.5, 0.5]
+    apart = np.array([-2.0, 0.5, 0.25], np.float32)              # for certain, whatever the scores
+    ids, w = check_route(rows, top_k=2, bias=apart, score="softmax")
+    assert ids.tolist() == [[1, 2]] * 4 and w[0].tolist() == [0.5, 0.5]
+    assert abs(w[1, 0].item() - 1 / (1 + math.exp(-1))) < 2 ** -18
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_weights_next_to_the_borders_of_fp32(score):
+    """Logits over the range in which fp32's exponentials become subnormal and vanish, chosen by widely spaced biases."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(12))
+    T, E = 300, 12
+    rows = (-rng.uniform(60.0, 115.0, (T, 1)) + rng.standard_normal((T, E))).astype(np.float32)
+    rows[:, 0] = 0.0 if score == "softmax" else -INF
+    bias = -np.arange(E).astype(np.float32)
+    bias[0] = -50.0
+    check_route(torch.from_numpy(rows).cuda(), top_k=5, bias=bias, score=score)
+
+
+def test_a_scale_of_scores_below_the_smallest_fp32_numbers():
+    """Not divided by their sum: scores of 2^-130 have all their bits once a scale brings them back into range."""
+    from paper_2310_09259_amd import api
+    rows = _logits([[-90.0, -91.0, -INF, -95.0]])
+    _, w = api.quik_moe_route(rows, 3, score="sigmoid", renormalize=False, scale=2.0 ** 120)
+    for got, l in zip(w[0].tolist(), (-90.0, -91.0, -95.0)):
+        ref = 2.0 ** 120 / (1.0 + math.exp(-l))
+        assert abs(got - ref) <= 2.0 ** -22 * ref
