@@ -235,7 +235,7 @@ __device__ __forceinline__ bool route_token(const MoeRouteArgs& a, int t, const 
     if (lane < a.top_k) {
         if (a.renormalize) mine = sum > 0 ? mine / sum : (F)0;
         a.ids[(size_t)t * a.top_k + lane] = id;
-        a.weights[(size_t)t * a.top_k + lane] = (float)(mine * (F)a.scale);
+        a.weights[(size_t)t * a.top_k + lane] = id < 0 ? 0.0f : (float)(mine * (F)a.scale);   // (whatever the scale)
     }
     return true;
 }
