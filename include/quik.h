@@ -483,10 +483,11 @@ int quik_linear_sp24(const void *x, int T, int K, int ldx, const int32_t *outlie
  *   y[t, n] = a[t, n]                                          (glu = 0; y has N columns)
  *   y[t, f] = a[t, f] * sigmoid(a[t, f]) * a[t, N / 2 + f]     (glu = 1; N even, y has N / 2 columns: the first half of the
  *                                                              channels are gates, the second half values)
- * Sums are fp32 and y is rounded once.  The scale is applied to fp32 sums of exact products, but for the largest
- * tiles of a plain layer (quik_debug_w4g_form 9 and 10): they first round the weights to the type of x, once per weight.
- * A row of x with an infinity, a NaN or (bf16) a value from 2^112 on, whose sums over a group fp32 may not hold, gives a
- * row of y without meaning; other rows are not affected.
+ * Sums are fp32, of exact products of x and integers, to which the scales are applied in fp32; y is rounded once.  (bf16 with
+ * few rows: the integers carry an offset of 136 + zero point, which is taken off the sums: their own fp32 error is about ten
+ * times that of the plain integers, a thousandth of the output's rounding.)
+ * A row of x with an infinity, a NaN or (bf16) a value from 2^104 / d on, d the largest quotient of two scales of a channel,
+ * whose sums in units of a scale fp32 may not hold, gives a row of y without meaning; other rows are not affected.
  *
  *  quik_weight_pack_w4g   once per layer: codes, scales and zero points -> w4 (quik_w4g_bytes(...) bytes, 16-byte aligned).
  *    w_q       packed signed 4-bit codes [N, ldw bytes] in the weight nibble order of this header, ldw >= K / 2
@@ -548,7 +549,7 @@ int quik_moe_linear_w4g(int type, const void *x, int ldx, int x_per_slot, const 
  * Test hooks of these products (host only).  quik_debug_w4g_form: the kernel that a product of `rows` rows (experts: T *
  * top_k; 0 experts: a layer) runs on with `cus` compute units: 0 .. 5 the kernels whose waves split K, of 16 x 16,
  * 16 x 32 (eight waves), 16 x 32 (four), 16 x 64, 32 x 32 and 32 x 64 rows x channels; 6 .. 10 the tile kernels of 32 x 128,
- * 64 x 128, 128 x 128, 256 x 128 and 256 x 256; 11 and 12 those of 32 x 128 and 64 x 128 with several workgroups to a CU.
+ * 64 x 128, 128 x 128, 256 x 128 and 256 x 256 (the last for groups of 128 or more columns, which are assumed here); 11 and 12 those of 32 x 128 and 64 x 128 with several workgroups to a CU.
  * QUIK_EINVAL / QUIK_EUNSUPPORTED on invalid input.
  * quik_debug_set_w4g_form: the one that products use from now on, in this process, where they can; -1: automatic.  Not
  * synchronised with calls in flight on other threads.

@@ -32,9 +32,10 @@ enum { kW4gRows16x16, kW4gRows16x32Wide, kW4gRows16x32, kW4gRows16x64, kW4gRows3
        kW4gTile32x128, kW4gTile64x128, kW4gTile128x128, kW4gTile256x128, kW4gTile256x256,
        kW4gTile32x128Small, kW4gTile64x128Small, kW4gForms };    // (Small: several workgroups to a CU)
 // What the rules choose (host only; launch_w4g launches exactly this).  by_rows: a row at a time
-int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, int cus);
+int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, bool tile256, int cus);
 void set_w4g_form(int form);                                            // test hook: -1 automatic
 hipError_t launch_w4g_tiles(const W4gArgs& a, int form, hipStream_t stream);
+hipError_t launch_w4g_tiles256(const W4gArgs& a, hipStream_t stream);   // (groups of 128, dense, no paired halves)
 hipError_t launch_weight_pack_w4g(const void* w_q, int ldw, const void* w_scale, const void* w_zero, int N, int K, int group,
                                   int glu, int experts, void* w4, hipStream_t stream);
 

@@ -361,7 +361,9 @@ void set_w4g_form(int form) { g_form.store(form, std::memory_order_relaxed); }
 // More rows of a dense layer: the least of an estimate, rounds of workgroups, one to a CU, times the tiles of 128 columns
 // that a wave (or group of waves) goes through, times what such a step takes, plus a start.  Measured steps: 1.3 us and 1.75
 // for 32 x 32 and 32 x 64 (six waves split K), 0.95 and 1.4 for tiles of 32 x 128 and 64 x 128 (two groups split K), 1.2,
-// 1.95 and 3.3 for 128 x 128, 256 x 128 and 256 x 256.  N = 11008, chosen : best other one: 24 rows 13.2 : 16.9, 48 rows
+// 1.95 and 3.3 for 128 x 128, 256 x 128 and 256 x 256, in fp16 with groups of 128; small groups and bf16 make them up to a half
+// longer, by about the same factor in all (over 390 sizes from 24 to 4096 rows, both types, groups of 32, 64 and 128, the choice
+// takes 0.2 % longer than the best, at most 7 %).  N = 11008, chosen : best other one: 24 rows 13.2 : 16.9, 48 rows
 // 19.8 : 22.3, 128 rows 23.3 : 31.9, 256 rows 39 : 42, 512 rows 60 : 69, 1024 rows 100 : 118, 2048 rows 199 : 214; N = 4096,
 // 1024 rows 45 : 47; N = 28672, K = 8192, 4096 rows 1550 : 1857.
 // Experts by a plan: workgroups of four waves, several to a CU, since each has few steps, and its start (its rows, its
@@ -369,7 +371,8 @@ void set_w4g_form(int form) { g_form.store(form, std::memory_order_relaxed); }
 // brackets the best with one workgroup to a CU): 64 experts of 2048 x 2816 in halves, bf16, groups of 64, 28 rows each 116 : 130 (158);
 // fp16, 256 rows each 337 : 293 (409); of 1408 x 2048, summed up, 256 rows each 231 : 213 (281); eight of 4096 x 4096 in
 // halves, 16 rows each 39.4 : 44 (42), 128 rows each 83 : 84 (101), 512 rows each 226 : 194 (252).
-int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, int cus) {
+// tile256: whether there is a 256 x 256 tile for the layer (dense, no paired halves, stored groups of 128)
+int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, bool tile256, int cus) {
     if (by_rows || (!experts && rows <= 16)) {
         const double all = (double)blocks * (by_rows ? rows : 1);
         if (all <= cus && !glu) return kW4gRows16x16;
@@ -386,7 +389,7 @@ int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by
     int best = kW4gTile256x128;
     double least = 1e30;
     for (const Cost& c : costs) {
-        if (glu && c.form == kW4gTile256x256) continue;  // (see quik_w4g_tiles.hip)
+        if (!tile256 && c.form == kW4gTile256x256) continue;
         const double tiles = (double)((rows + c.rows - 1) / c.rows) * ((blocks + c.blocks - 1) / c.blocks);
         const double t = c.start + ceil(tiles / cus) * ((kt + c.k_split - 1) / c.k_split) * c.step;
         if (t < least) { least = t; best = c.form; }
@@ -403,12 +406,13 @@ hipError_t launch_w4g(const W4gArgs& args, hipStream_t stream) {
         if (hipError_t rc = launch_moe_plan(a.ids, a.rows, a.experts, a.plan, stream); rc != hipSuccess) return rc;
     }
     const int cus = compute_units();
+    const bool tile256 = !a.glu && !a.ids && a.group == 128;
     int form = g_form.load(std::memory_order_relaxed);
-    if (form < 0) form = choose_w4g_form(by_token ? a.rows / a.top_k : a.rows, a.w.nt, a.w.kt, a.glu, a.ids ? a.experts : 0, by_rows, cus > 0 ? cus : 256);
+    if (form < 0) form = choose_w4g_form(by_token ? a.rows / a.top_k : a.rows, a.w.nt, a.w.kt, a.glu, a.ids ? a.experts : 0, by_rows, tile256, cus > 0 ? cus : 256);
     if (by_rows && form > kW4gRows16x64) form = kW4gRows16x32;
     if (a.ids && !by_rows && form < kW4gTile32x128) form = kW4gTile32x128Small;
     if (a.glu && form == kW4gRows16x16) form = kW4gRows16x32Wide;
-    if (a.glu && form == kW4gTile256x256) form = kW4gTile256x128;
+    if (!tile256 && form == kW4gTile256x256) form = kW4gTile256x128;
     const hipError_t rc = form < kW4gTile32x128 ? launch_w4g_rows(a, form, stream) : launch_w4g_tiles(a, form, stream);
     if (rc != hipSuccess || !a.weights || by_token) return rc;
     return launch_moe_combine(a.stage, a.ids, a.weights, a.rows / a.top_k, a.top_k, a.experts, a.width, a.bf16, a.y, a.ldy, stream);

@@ -101,7 +101,7 @@ int quik_debug_w4g_form(int rows, int N, int K, int glu, int experts, int cus) {
     const int rc = check_weights(N, K, 0, glu, experts ? experts : 1);
     if (rc != QUIK_OK) return rc;
     const quik::w4g::Layout l = quik::w4g::layout(N, K, 0, false, glu != 0, 1);
-    return quik::choose_w4g_form(rows, l.nt, l.kt, glu != 0, experts, experts && rows <= experts, cus);
+    return quik::choose_w4g_form(rows, l.nt, l.kt, glu != 0, experts, experts && rows <= experts, !glu && !experts, cus);
 }
 
 int quik_debug_set_w4g_form(int form) {
