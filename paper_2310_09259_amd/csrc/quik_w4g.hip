@@ -342,7 +342,7 @@ hipError_t launch_weight_pack_w4g(const void* w_q, int ldw, const void* w_scale,
     const Layout l = layout(N, K, group, w_zero != nullptr, glu != 0, experts);
     uint8_t* const base = static_cast<uint8_t*>(w4);
     PackArgs a{static_cast<const uint8_t*>(w_q), ldw, static_cast<const uint16_t*>(w_scale), static_cast<const int8_t*>(w_zero),
-               N, K, group ? (K + group - 1) / group : 1, group ? group : K, l.kg, glu, l.nt, l.kt,
+               N, K, group ? (K - 1) / group + 1 : 1, group ? group : K, l.kg, glu, l.nt, l.kt,   // (a group may be near 2^31)
                reinterpret_cast<uint32_t*>(base), reinterpret_cast<uint16_t*>(base + l.scales_at),
                reinterpret_cast<int8_t*>(base + l.zeros_at)};
     hipLaunchKernelGGL(pack_w4g_kernel, dim3(l.nt * l.kt, experts), dim3(256), 0, stream, a);
