@@ -40,7 +40,8 @@ __device__ __forceinline__ int channel_of(int b, int l, int N, int glu) {
 __global__ __launch_bounds__(256) void pack_w4g_kernel(PackArgs a) {
     const int tiles = a.nt * a.kt;
     const size_t e = blockIdx.y;
-    const int tile = blockIdx.x, b = tile / a.kt, kt = tile % a.kt;
+    const int tile = blockIdx.z * gridDim.x + blockIdx.x, b = tile / a.kt, kt = tile % a.kt;
+    if (tile >= tiles) return;
     {
         const int lane = threadIdx.x >> 2, s = threadIdx.x & 3;
         const int n = channel_of(b, lane & 15, a.N, a.glu), k = kt * kCols + s * 32 + (lane >> 4) * 8;
@@ -345,7 +346,9 @@ hipError_t launch_weight_pack_w4g(const void* w_q, int ldw, const void* w_scale,
                N, K, group ? (K - 1) / group + 1 : 1, group ? group : K, l.kg, glu, l.nt, l.kt,   // (a group may be near 2^31)
                reinterpret_cast<uint32_t*>(base), reinterpret_cast<uint16_t*>(base + l.scales_at),
                reinterpret_cast<int8_t*>(base + l.zeros_at)};
-    hipLaunchKernelGGL(pack_w4g_kernel, dim3(l.nt * l.kt, experts), dim3(256), 0, stream, a);
+    // up to 2^16 x 2^8 tiles of 256 threads: more than a grid's x takes
+    const int tiles = l.nt * l.kt, slices = (tiles - 1) / (1 << 23) + 1;
+    hipLaunchKernelGGL(pack_w4g_kernel, dim3((tiles - 1) / slices + 1, experts, slices), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
