@@ -547,14 +547,16 @@ int quik_moe_linear_w4g(int type, const void *x, int ldx, int x_per_slot, const 
 
 /*
  * Test hooks of these products (host only).  quik_debug_w4g_form: the kernel that a product of `rows` rows (experts: T *
- * top_k; 0 experts: a layer) runs on with `cus` compute units: 0 .. 5 the kernels whose waves split K, of 16 x 16,
+ * top_k, without weights; 0 experts: a layer) runs on with `cus` compute units: 0 .. 5 the kernels whose waves split K, of 16 x 16,
  * 16 x 32 (eight waves), 16 x 32 (four), 16 x 64, 32 x 32 and 32 x 64 rows x channels; 6 .. 10 the tile kernels of 32 x 128,
  * 64 x 128, 128 x 128, 256 x 128 and 256 x 256 (the last for groups of 128 or more columns, which are assumed here); 11 and 12 those of 32 x 128 and 64 x 128 with several workgroups to a CU.
  * QUIK_EINVAL / QUIK_EUNSUPPORTED on invalid input.
+ * quik_debug_moe_w4g_form: that of quik_moe_linear_w4g (combine: with weights).
  * quik_debug_set_w4g_form: the one that products use from now on, in this process, where they can; -1: automatic.  Not
  * synchronised with calls in flight on other threads.
  */
 int quik_debug_w4g_form(int rows, int N, int K, int glu, int experts, int cus);
+int quik_debug_moe_w4g_form(int T, int top_k, int N, int K, int group, int glu, int experts, int combine, int cus);
 int quik_debug_set_w4g_form(int form);
 
 /*

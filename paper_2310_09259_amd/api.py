@@ -128,6 +128,8 @@ def load() -> C.CDLL:
         lib.quik_linear_w4g.argtypes = [i, vp, i, i, i, vp, i, i, i, vp, i, vp, i, vp]
         lib.quik_debug_w4g_form.restype = i
         lib.quik_debug_w4g_form.argtypes = [i, i, i, i, i, i]
+        lib.quik_debug_moe_w4g_form.restype = i
+        lib.quik_debug_moe_w4g_form.argtypes = [i, i, i, i, i, i, i, i, i]
         lib.quik_debug_set_w4g_form.restype = i
         lib.quik_debug_set_w4g_form.argtypes = [i]
         lib.quik_moe_route.restype = i
@@ -1062,6 +1064,15 @@ def quik_debug_w4g_form(rows: int, N: int, K: int, glu: bool = False, experts: i
     form = load().quik_debug_w4g_form(rows, N, K, int(glu), experts, cus)
     if form < 0:
         _check(form, "quik_debug_w4g_form")
+    return form
+
+
+def quik_debug_moe_w4g_form(T: int, top_k: int, N: int, K: int, group: int, experts: int, glu: bool = False,
+                            combine: bool = False, cus: int = 256) -> int:
+    """Host-only: the kernel of quik_moe_linear_w4g (combine: with weights)."""
+    form = load().quik_debug_moe_w4g_form(T, top_k, N, K, group, int(glu), experts, int(combine), cus)
+    if form < 0:
+        _check(form, "quik_debug_moe_w4g_form")
     return form
 
 

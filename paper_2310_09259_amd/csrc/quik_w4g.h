@@ -31,8 +31,14 @@ hipError_t launch_w4g(const W4gArgs& a, hipStream_t stream);
 enum { kW4gRows16x16, kW4gRows16x32Wide, kW4gRows16x32, kW4gRows16x64, kW4gRows32x32, kW4gRows32x64,
        kW4gTile32x128, kW4gTile64x128, kW4gTile128x128, kW4gTile256x128, kW4gTile256x256,
        kW4gTile32x128Small, kW4gTile64x128Small, kW4gForms };    // (Small: several workgroups to a CU)
-// What the rules choose (host only; launch_w4g launches exactly this).  by_rows: a row at a time
-int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, bool tile256, int cus);
+// What a product runs on (host only; launch_w4g launches exactly this): top_k, combine: experts' slots to a token, with weights;
+// group: the stored one; experts: 0 for a dense layer
+struct W4gChoice {
+    int form;
+    bool by_rows;                 // experts: a row at a time, without a plan
+    bool by_token;                // of those: a token and the sum of its slots at a time
+};
+W4gChoice resolve_w4g(int rows, int top_k, bool combine, int blocks, int kt, int group, bool glu, int experts, int cus);
 void set_w4g_form(int form);                                            // test hook: -1 automatic
 hipError_t launch_w4g_tiles(const W4gArgs& a, int form, hipStream_t stream);
 hipError_t launch_w4g_tiles256(const W4gArgs& a, hipStream_t stream);   // (groups of 128, dense, no paired halves)

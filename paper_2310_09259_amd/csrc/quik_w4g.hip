@@ -375,7 +375,7 @@ void set_w4g_form(int form) { g_form.store(form, std::memory_order_relaxed); }
 // fp16, 256 rows each 337 : 293 (409); of 1408 x 2048, summed up, 256 rows each 231 : 213 (281); eight of 4096 x 4096 in
 // halves, 16 rows each 39.4 : 44 (42), 128 rows each 83 : 84 (101), 512 rows each 226 : 194 (252).
 // tile256: whether there is a 256 x 256 tile for the layer (dense, no paired halves, stored groups of 128)
-int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, bool tile256, int cus) {
+static int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, bool tile256, int cus) {
     if (by_rows || (!experts && rows <= 16)) {
         const double all = (double)blocks * (by_rows ? rows : 1);
         if (all <= cus && !glu) return kW4gRows16x16;
@@ -400,24 +400,32 @@ int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by
     return best;
 }
 
+W4gChoice resolve_w4g(int rows, int top_k, bool combine, int blocks, int kt, int group, bool glu, int experts, int cus) {
+    // a row (or a token and its slots) at a time where hardly two rows share an expert: no plan, no sums in memory
+    W4gChoice c;
+    c.by_rows = experts && rows <= experts;
+    c.by_token = c.by_rows && combine && !glu;
+    const bool tile256 = !glu && !experts && group == 128;
+    c.form = g_form.load(std::memory_order_relaxed);
+    if (c.form < 0) c.form = choose_w4g_form(c.by_token ? rows / top_k : rows, blocks, kt, glu, experts, c.by_rows, tile256, cus);
+    // (a form that was set may not be one for this product)
+    if (c.by_rows && c.form > kW4gRows16x64) c.form = kW4gRows16x32;
+    if (experts && !c.by_rows && c.form < kW4gTile32x128) c.form = kW4gTile32x128Small;
+    if (glu && c.form == kW4gRows16x16) c.form = kW4gRows16x32Wide;
+    if (!tile256 && c.form == kW4gTile256x256) c.form = kW4gTile256x128;
+    return c;
+}
+
 hipError_t launch_w4g(const W4gArgs& args, hipStream_t stream) {
     W4gArgs a = args;
-    // a row (or a token and its slots) at a time where hardly two rows share an expert: no plan, no sums in memory
-    const bool by_rows = a.ids && a.rows <= a.experts, by_token = by_rows && a.weights && !a.glu;
-    if (by_rows) a.plan = nullptr;
+    const int cus = compute_units();
+    const W4gChoice c = resolve_w4g(a.rows, a.top_k, a.weights != nullptr, a.w.nt, a.w.kt, a.group, a.glu, a.ids ? a.experts : 0, cus > 0 ? cus : 256);
+    if (c.by_rows) a.plan = nullptr;
     else if (a.ids) {
         if (hipError_t rc = launch_moe_plan(a.ids, a.rows, a.experts, a.plan, stream); rc != hipSuccess) return rc;
     }
-    const int cus = compute_units();
-    const bool tile256 = !a.glu && !a.ids && a.group == 128;
-    int form = g_form.load(std::memory_order_relaxed);
-    if (form < 0) form = choose_w4g_form(by_token ? a.rows / a.top_k : a.rows, a.w.nt, a.w.kt, a.glu, a.ids ? a.experts : 0, by_rows, tile256, cus > 0 ? cus : 256);
-    if (by_rows && form > kW4gRows16x64) form = kW4gRows16x32;
-    if (a.ids && !by_rows && form < kW4gTile32x128) form = kW4gTile32x128Small;
-    if (a.glu && form == kW4gRows16x16) form = kW4gRows16x32Wide;
-    if (!tile256 && form == kW4gTile256x256) form = kW4gTile256x128;
-    const hipError_t rc = form < kW4gTile32x128 ? launch_w4g_rows(a, form, stream) : launch_w4g_tiles(a, form, stream);
-    if (rc != hipSuccess || !a.weights || by_token) return rc;
+    const hipError_t rc = c.form < kW4gTile32x128 ? launch_w4g_rows(a, c.form, stream) : launch_w4g_tiles(a, c.form, stream);
+    if (rc != hipSuccess || !a.weights || c.by_token) return rc;
     return launch_moe_combine(a.stage, a.ids, a.weights, a.rows / a.top_k, a.top_k, a.experts, a.width, a.bf16, a.y, a.ldy, stream);
 }
 

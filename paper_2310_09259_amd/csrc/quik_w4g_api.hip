@@ -101,7 +101,17 @@ int quik_debug_w4g_form(int rows, int N, int K, int glu, int experts, int cus) {
     const int rc = check_weights(N, K, 0, glu, experts ? experts : 1);
     if (rc != QUIK_OK) return rc;
     const quik::w4g::Layout l = quik::w4g::layout(N, K, 0, false, glu != 0, 1);
-    return quik::choose_w4g_form(rows, l.nt, l.kt, glu != 0, experts, experts && rows <= experts, !glu && !experts, cus);
+    return quik::resolve_w4g(rows, 1, false, l.nt, l.kt, l.kg, glu != 0, experts, cus).form;
+}
+
+int quik_debug_moe_w4g_form(int T, int top_k, int N, int K, int group, int glu, int experts, int combine, int cus) {
+    int rc = check_slots(T, top_k, experts);
+    if (rc != QUIK_OK) return rc;
+    if ((combine != 0 && combine != 1) || cus <= 0) return QUIK_EINVAL;
+    rc = check_weights(N, K, group, glu, experts);
+    if (rc != QUIK_OK) return rc;
+    const quik::w4g::Layout l = quik::w4g::layout(N, K, group, false, glu != 0, 1);
+    return quik::resolve_w4g(T * top_k, top_k, combine != 0, l.nt, l.kt, l.kg, glu != 0, experts, cus).form;
 }
 
 int quik_debug_set_w4g_form(int form) {
