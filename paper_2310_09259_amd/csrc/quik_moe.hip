@@ -336,7 +336,7 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const float* stage, co
                                                           int experts, int width, void* y, int ldy) {
     asm volatile("" ::: "v63");                          // a whole share of the register file (see quik_gemm.hip)
     const int per_row = (width + 3) / 4;
-    const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t at = ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
     if (at >= (size_t)T * per_row) return;
     const size_t t = at / per_row;
     const int n = (int)(at % per_row) * 4, count = min(4, width - n);
@@ -381,7 +381,9 @@ hipError_t launch_moe_plan(const int32_t* ids, int rows, int experts, int32_t* p
 
 hipError_t launch_moe_combine(const float* stage, const int32_t* ids, const float* weights, int T, int top_k, int experts,
                               int width, int bf16, void* y, int ldy, hipStream_t stream) {
-    const dim3 grid((unsigned)(((size_t)T * ((width + 3) / 4) + 255) / 256)), threads(256);
+    // (a grid's x dimension takes less than 2^32 threads)
+    const size_t blocks = ((size_t)T * ((width + 3) / 4) + 255) / 256, slices = (blocks - 1) / (1 << 23) + 1;
+    const dim3 grid((unsigned)((blocks - 1) / slices + 1), (unsigned)slices), threads(256);
     if (bf16) hipLaunchKernelGGL(moe_combine_kernel<Bf16>, grid, threads, 0, stream, stage, ids, weights, T, top_k, experts, width, y, ldy);
     else hipLaunchKernelGGL(moe_combine_kernel<Half>, grid, threads, 0, stream, stage, ids, weights, T, top_k, experts, width, y, ldy);
     return hipGetLastError();

@@ -46,3 +46,27 @@ def test_the_widest_and_deepest_layer():
         xs = x.double().cpu().numpy()
         ref, tol = xs @ W.T, 2.0 ** -24 * (K + 8) * (np.abs(xs) @ np.abs(W).T)
         assert np.all(np.abs(y - ref) <= STEP["float16"] * (np.abs(ref) + tol) + tol + TINY["float16"]), T
+
+
+def test_a_weighted_sum_of_2_to_the_34_outputs():
+    """2^17 tokens of one slot and 2^17 channels: 2^32 groups of four columns to add up, 69 GB of sums in memory."""
+    import torch
+    from paper_2310_09259_amd import api
+    T, K, N, E = 1 << 17, 128, 1 << 17, 2
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        torch.cuda.empty_cache()
+    raw = layer(4, N, K, 128, False, experts=E)
+    w = pack(raw, K, 128)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn((T, K), generator=gen, device="cuda").half()
+    ids = torch.randint(0, E, (T, 1), generator=gen, device="cuda", dtype=torch.int32)
+    weights = torch.rand((T, 1), generator=gen, device="cuda")
+    y = api.quik_moe_linear_w4g(x, ids, w, weights=weights)
+    for t in (0, 1, T // 2, T - 2, T - 1):
+        ref = x[t].double().cpu().numpy() @ raw[3][ids[t, 0].item()].T * weights[t, 0].item()
+        mag = np.abs(x[t].double().cpu().numpy()) @ np.abs(raw[3][ids[t, 0].item()]).T * weights[t, 0].item()
+        tol = 2.0 ** -24 * (K + 16) * mag
+        got = y[t].double().cpu().numpy()
+        assert np.all(np.abs(got - ref) <= STEP["float16"] * (np.abs(ref) + tol) + tol + TINY["float16"]), t
+    del y
+    torch.cuda.empty_cache()
