@@ -499,8 +499,8 @@ int quik_linear_sp24(const void *x, int T, int K, int ldx, const int32_t *outlie
  *                         those that w4 was packed with.  One kernel launch, no workspace.
  *
  * Limits of these layers: T >= 1; K a multiple of 8, at most 32768; N at most 2^20; x and w4 16-byte aligned, ldx a
- * multiple of 8, at most 2^22; scales and zero points of a layer (of all its experts) below 3.75 GB; ldy >= the columns of
- * y, y otherwise unconstrained; w_q 16-byte aligned, ldw a multiple of 16.  y does not overlap an input.
+ * multiple of 8, at most 2^22; scales and zero points of a layer (of all its experts) below 3.75 GB; fewer threads than 2^32
+ * (products of fewer than 2^30 sums always are); ldy >= the columns of y, y otherwise unconstrained; w_q 16-byte aligned, ldw a multiple of 16.  y does not overlap an input.
  */
 size_t quik_w4g_bytes(int N, int K, int group, int has_zero, int glu, int experts);
 int quik_weight_pack_w4g(const void *w_q, int ldw, const void *w_scale, const void *w_zero, int N, int K, int group, int glu,

@@ -25,7 +25,7 @@ struct W4gArgs {
     const float* weights;         // [rows]: y is [T], the weighted sum of a token's slots; or null: y is [rows]
     float* stage;                 // [rows][width] for the sum, where the rows are computed one by one
 };
-hipError_t launch_w4g(const W4gArgs& a, hipStream_t stream);
+hipError_t launch_w4g(const W4gArgs& a, hipStream_t stream);   // hipErrorInvalidConfiguration: more threads than a grid takes
 // The kernels a product can run on: rows x channels of a workgroup's tile.  kW4gRows...: the waves split K (quik_w4g.hip);
 // kW4gTile...: quik_w4g_tiles.hip
 enum { kW4gRows16x16, kW4gRows16x32Wide, kW4gRows16x32, kW4gRows16x64, kW4gRows32x32, kW4gRows32x64,

@@ -416,10 +416,23 @@ W4gChoice resolve_w4g(int rows, int top_k, bool combine, int blocks, int kt, int
     return c;
 }
 
+// (what a grid's x dimension takes is counted in threads)
+static bool fits_a_grid(const W4gArgs& a, const W4gChoice& c) {
+    static const struct { int rows, blocks, threads; } tile[kW4gForms] = {
+        {16, 1, 512}, {16, 2, 512}, {16, 2, 256}, {16, 4, 256}, {32, 2, 384}, {32, 4, 384},
+        {32, 8, 512}, {64, 8, 512}, {128, 8, 512}, {256, 8, 512}, {256, 16, 512}, {32, 8, 256}, {64, 8, 256}};
+    const auto& t = tile[c.form];
+    const size_t groups = (a.w.nt + t.blocks - 1) / t.blocks;
+    const size_t rows = c.by_token ? a.rows / a.top_k : c.by_rows ? a.rows
+                        : a.ids ? a.rows / t.rows + min(a.rows, a.experts + 1) : (a.rows + t.rows - 1) / t.rows;
+    return rows * groups * t.threads <= 0xFFFFFFFFu;
+}
+
 hipError_t launch_w4g(const W4gArgs& args, hipStream_t stream) {
     W4gArgs a = args;
     const int cus = compute_units();
     const W4gChoice c = resolve_w4g(a.rows, a.top_k, a.weights != nullptr, a.w.nt, a.w.kt, a.group, a.glu, a.ids ? a.experts : 0, cus > 0 ? cus : 256);
+    if (!fits_a_grid(a, c)) return hipErrorInvalidConfiguration;
     if (c.by_rows) a.plan = nullptr;
     else if (a.ids) {
         if (hipError_t rc = launch_moe_plan(a.ids, a.rows, a.experts, a.plan, stream); rc != hipSuccess) return rc;

@@ -16,6 +16,8 @@ constexpr size_t kMaxOffset = 0xF0000000u;
 
 inline bool aligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 inline int status(hipError_t rc) { return rc == hipSuccess ? QUIK_OK : QUIK_ELAUNCH; }
+// of a product, which refuses what no grid holds before it launches anything
+inline int product_status(hipError_t rc) { return rc == hipErrorInvalidConfiguration ? QUIK_EUNSUPPORTED : status(rc); }
 inline size_t up256(size_t v) { return (v + 255u) & ~size_t(255); }
 
 int check_weights(int N, int K, int group, int glu, int experts) {
@@ -93,7 +95,7 @@ int quik_linear_w4g(int type, const void* x, int T, int K, int ldx, const void* 
     if (rc != QUIK_OK) return rc;
     quik::W4gArgs a = product(type, x, ldx, w4, group, has_zero, glu, bias, N, K, 1, y, ldy);
     a.rows = T;
-    return status(quik::launch_w4g(a, static_cast<hipStream_t>(stream)));
+    return product_status(quik::launch_w4g(a, static_cast<hipStream_t>(stream)));
 }
 
 int quik_debug_w4g_form(int rows, int N, int K, int glu, int experts, int cus) {
@@ -164,7 +166,7 @@ int quik_moe_linear_w4g(int type, const void* x, int ldx, int x_per_slot, const 
     a.weights = weights;
     a.plan = reinterpret_cast<int32_t*>(base + m.plan);
     a.stage = weights ? reinterpret_cast<float*>(base + m.stage) : nullptr;
-    return status(quik::launch_w4g(a, static_cast<hipStream_t>(stream)));
+    return product_status(quik::launch_w4g(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"
