@@ -484,8 +484,8 @@ int quik_linear_sp24(const void *x, int T, int K, int ldx, const int32_t *outlie
  *   y[t, f] = a[t, f] * sigmoid(a[t, f]) * a[t, N / 2 + f]     (glu = 1; N even, y has N / 2 columns: the first half of the
  *                                                              channels are gates, the second half values)
  * Sums are fp32, of exact products of x and integers, to which the scales are applied in fp32; y is rounded once.  (bf16 with
- * few rows: the integers carry an offset of 136 + zero point, which is taken off the sums: their own fp32 error is about ten
- * times that of the plain integers, a thousandth of the output's rounding.)
+ * few rows: the integers carry an offset of 136 + zero point, which is taken off the sums: their own fp32 error is ten to
+ * twenty times that of the plain integers, a thousandth of the output's rounding.)
  * A row of x with an infinity, a NaN or (bf16) a value from 2^104 / d on, d the largest quotient of two scales of a channel,
  * whose sums in units of a scale fp32 may not hold, gives a row of y without meaning; other rows are not affected.
  *
@@ -519,7 +519,8 @@ int quik_linear_w4g(int type, const void *x, int T, int K, int ldx, const void *
  *      ids[t, :]     = the top_k experts of the largest choices, largest first       int32 [T, top_k]
  *      weights[t, :] = their scores, divided by their sum if `renormalize` (by nothing, and 0, if that is 0), times `scale`
  *                                                                                    fp32 [T, top_k]
- *    Ties go to the lowest index; choices are told apart as float64 tells them.  An expert whose logit is -infinity or NaN,
+ *    Ties go to the lowest index; choices are told apart as float64 tells them, and scores are what float64 makes of them (a
+ *    sigmoid below e^-709 is 0), weights good to fp32.  An expert whose logit is -infinity or NaN,
  *    or whose choice is, takes no part (an infinite logit is the limit: the softmax is shared among those).  A slot that no
  *    expert is left for gets id -1 and weight 0.
  *    Limits: experts <= 1024, top_k <= 32, groups <= 64, group_top <= experts / groups, top_k <= topk_groups * experts / groups.
@@ -528,8 +529,8 @@ int quik_linear_w4g(int type, const void *x, int T, int K, int ldx, const void *
  *      a[r, n] = sum_k x[row, k] * W_e[n, k] (+ bias[e, n])   and glu as above, where `row` is t (x_per_slot = 0: x is
  *                                                             [T, ldx]) or r (x_per_slot = 1: x is [T * top_k, ldx])
  *      y[r, :] = a[r, :]                                      weights NULL: y is [T * top_k, ldy]
- *      y[t, :] = sum_j weights[t, j] * a[t * top_k + j, :]    weights fp32 [T, top_k]: y is [T, ldy]; summed in fp32 in the
- *                                                             order of the slots, rounded once
+ *      y[t, :] = sum_j weights[t, j] * a[t * top_k + j, :]    weights fp32 [T, top_k]: y is [T, ldy]; summed in fp32 in a
+ *                                                             fixed order, rounded once
  *    An id outside 0 .. experts - 1 (padding, an expert that another GPU holds) is no expert: its rows of y are zeros,
  *    and it takes no part in a sum (its weight is not looked at).  The same expert twice in a token is two slots.
  *      bias        [experts, N] or NULL

@@ -365,15 +365,15 @@ void set_w4g_form(int form) { g_form.store(form, std::memory_order_relaxed); }
 // that a wave (or group of waves) goes through, times what such a step takes, plus a start.  Measured steps: 1.3 us and 1.75
 // for 32 x 32 and 32 x 64 (six waves split K), 0.95 and 1.4 for tiles of 32 x 128 and 64 x 128 (two groups split K), 1.2,
 // 1.95 and 3.3 for 128 x 128, 256 x 128 and 256 x 256, in fp16 with groups of 128; small groups and bf16 make them up to a half
-// longer, by about the same factor in all (over 390 sizes from 24 to 4096 rows, both types, groups of 32, 64 and 128, the choice
-// takes 0.2 % longer than the best, at most 7 %).  N = 11008, chosen : best other one: 24 rows 13.2 : 16.9, 48 rows
-// 19.8 : 22.3, 128 rows 23.3 : 31.9, 256 rows 39 : 42, 512 rows 60 : 69, 1024 rows 100 : 118, 2048 rows 199 : 214; N = 4096,
-// 1024 rows 45 : 47; N = 28672, K = 8192, 4096 rows 1550 : 1857.
+// longer, by about the same factor in all.  (256 x 256 has come to 3.6; over 390 sizes from 24 to 4096 rows, both types, groups of
+// 32, 64 and 128, the choice takes 0.2 % longer than the best of these kernels and at most 7 %, with 3.6 up to 13 %.)  N = 11008, chosen : best other one: 24 rows 14.3 : 17.4, 48 rows
+// 19.1 : 23.7, 128 rows 24.7 : 34, 256 rows 41.7 : 47.8, 512 rows 62 : 73, 1024 rows 113 : 126, 2048 rows 199 : 232; N = 4096,
+// 1024 rows 44.5 : 49.4; N = 28672, K = 8192, 4096 rows 1660 : 1870.
 // Experts by a plan: workgroups of four waves, several to a CU, since each has few steps, and its start (its rows, its
 // first tiles) and its end would leave the CU idle.  Tiles of 32 rows up to about a hundred rows to an expert, then of 64 (in
-// brackets the best with one workgroup to a CU): 64 experts of 2048 x 2816 in halves, bf16, groups of 64, 28 rows each 116 : 130 (158);
-// fp16, 256 rows each 337 : 293 (409); of 1408 x 2048, summed up, 256 rows each 231 : 213 (281); eight of 4096 x 4096 in
-// halves, 16 rows each 39.4 : 44 (42), 128 rows each 83 : 84 (101), 512 rows each 226 : 194 (252).
+// brackets the best with one workgroup to a CU): 64 experts of 2048 x 2816 in halves, bf16, groups of 64, 28 rows each 103 : 122 (150);
+// fp16, 256 rows each 345 : 295 (424); of 1408 x 2048, summed up, 256 rows each 232 : 205 (288); eight of 4096 x 4096 in
+// halves, 16 rows each 39.3 : 44 (42), 128 rows each 84 : 85 (105), 512 rows each 241 : 196 (256).
 // tile256: whether there is a 256 x 256 tile for the layer (dense, no paired halves, stored groups of 128)
 static int choose_w4g_form(int rows, int blocks, int kt, bool glu, int experts, bool by_rows, bool tile256, int cus) {
     if (by_rows || (!experts && rows <= 16)) {
