@@ -14,9 +14,9 @@
 //          group.
 //   else   (256 x 256, which has no room for that; groups of 128) the sums are in units of their channel's scale.  Where the next
 //          group begins they are multiplied by the quotient of the old scale and the new one, two roundings of 2^-24, and the
-//          units come off at the end.  Rows x channels of a wave at a time go pair of channel blocks by pair, the row blocks of
-//          a k-step staying in registers, so that weights widened ahead take a quarter of them.
-// For 4096 x 8192 x 28672 in fp16 : bf16, groups of 128, 256 x 256 takes 1660 : 1760 us and 256 x 128 1870 : 1970.
+//          units come off at the end.  A k-step goes through the channel blocks pair by pair, with all its row blocks in
+//          registers: the weights widened ahead are those of a pair, not of all blocks.
+// For 4096 x 8192 x 28672 in fp16 : bf16, groups of 128, 256 x 256 takes 1660 : 1790 us and 256 x 128 1880 : 2000.
 //
 // The activations of 128 columns go through LDS, two stages, copied without passing through registers; rows are 256
 // bytes, their sixteen 16-byte pieces exchanged by the row's number so that sixteen rows' pieces of one k fall into
@@ -72,7 +72,7 @@ template <> struct CodesOf<Bf16> { typedef Bf16Codes type; };
 
 // IB x JB blocks of 16 to a wave, WM x WN waves to a tile, KS groups of such waves that take every KS-th stage each and add
 // up through LDS at the end, in their order.  NST stages to a group: two where a stage is long enough to hide the next
-// one's way from memory (256 x 256: 2.9 us), three or four for the small tiles.  OCC waves per SIMD: two; four for the
+// one's way from memory (256 x 256: 3.7 us), three or four for the small tiles.  OCC waves per SIMD: two; four for the
 // smallest tile of experts, whose workgroups' starts and ends go on behind each other's products.
 template <typename TY, int KG, int IB, int JB, int WM, int WN, int KS, int NST, int OCC, bool FOLD>
 __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_tiles_kernel(W4gArgs a, int tiles_m) {
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
     const uint8_t* const scales = a.w.scales + e * a.w.scales_e;
     const uint8_t* const zeros = a.w.zeros ? a.w.zeros + e * a.w.zeros_e : scales;
     const uint32_t zero_mask = a.w.zeros ? 0xFFFFFFFFu : 0u;
-    const uint32_t lane_group = l16 * PER;
-    uint32_t sc[JB][(PER + 1) / 2], scn[JB][(PER + 1) / 2], ze[JB], zen[JB];
+    // of this stage and the next: zero points, PER of channel l16; not FOLD: the scale in the low half, the zero point above it
+    uint32_t sz[JB], scn[JB], zen[JB];
     // FOLD: the scales of channels 4 g .. 4 g + 3, whose sums this lane has, [4][PER]; of the next stage; of the last group
     uint32_t sf[JB][2 * PER] = {}, sfn[JB][2 * PER] = {};
     _Float16 sl[JB][4] = {};
@@ -176,40 +176,32 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
         if constexpr (!FOLD) {                           // (32-bit addresses)
             const uint32_t t = (uint32_t)min(wn * JB + j, a.w.nt - 1 - b0) * a.w.kt + (uint32_t)min(kt, a.w.kt - 1);
             const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(s0), 0, kRange, 0x00020000);
-            scn[j][0] = __builtin_amdgcn_raw_buffer_load_b16(r, lane_group * 2, t * (kBlock * 2), 0);
-            zen[j] = __builtin_amdgcn_raw_buffer_load_b8(r, lane_group, zeros_at + t * kBlock, 0);
-            return;
-        }
-        const size_t tile = (size_t)min(b0 + wn * JB + j, a.w.nt - 1) * a.w.kt + min(kt * KS + kg, a.w.kt - 1);
-        const uint8_t* s = scales + tile * (kBlock * PER * 2) + lane_group * 2;
-        if constexpr (FOLD) {
+            scn[j] = __builtin_amdgcn_raw_buffer_load_b16(r, l16 * 2, t * (kBlock * 2), 0);
+            zen[j] = __builtin_amdgcn_raw_buffer_load_b8(r, l16, zeros_at + t * kBlock, 0);
+        } else {
+            const size_t tile = (size_t)min(b0 + wn * JB + j, a.w.nt - 1) * a.w.kt + min(kt * KS + kg, a.w.kt - 1);
             const uint2* f = reinterpret_cast<const uint2*>(scales + tile * (kBlock * PER * 2) + (uint32_t)g * (8 * PER));
 #pragma unroll
             for (int q = 0; q < PER; ++q) { const uint2 v = f[q]; sfn[j][2 * q] = v.x; sfn[j][2 * q + 1] = v.y; }
-        } else if constexpr (PER == 1) scn[j][0] = *reinterpret_cast<const uint16_t*>(s);
-        else if constexpr (PER == 2) scn[j][0] = *reinterpret_cast<const uint32_t*>(s);
-        else { const uint2 v = *reinterpret_cast<const uint2*>(s); scn[j][0] = v.x; scn[j][1] = v.y; }
-        const uint8_t* z = zeros + tile * (kBlock * PER) + lane_group;
-        if constexpr (PER == 1) zen[j] = *z;
-        else if constexpr (PER == 2) zen[j] = *reinterpret_cast<const uint16_t*>(z);
-        else zen[j] = *reinterpret_cast<const uint32_t*>(z);
+            const uint8_t* z = zeros + tile * (kBlock * PER) + (uint32_t)(l16 * PER);
+            if constexpr (PER == 1) zen[j] = *z;
+            else if constexpr (PER == 2) zen[j] = *reinterpret_cast<const uint16_t*>(z);
+            else zen[j] = *reinterpret_cast<const uint32_t*>(z);
+        }
     };
     auto take = [&](uint32_t slot) {
 #pragma unroll
         for (int j = 0; j < JB; ++j) {
             if constexpr (S_LDS) {
-                const uint8_t* const at = lds + slot + S_AT + (wn * JB + j) * (64 * PER);
-                if constexpr (FOLD) ;
-                else if constexpr (PER == 1) sc[j][0] = *reinterpret_cast<const uint16_t*>(at + l16 * 2);
-                else if constexpr (PER == 2) sc[j][0] = *reinterpret_cast<const uint32_t*>(at + l16 * 4);
-                else { const uint2 v = *reinterpret_cast<const uint2*>(at + l16 * 8); sc[j][0] = v.x; sc[j][1] = v.y; }
-                if constexpr (PER == 1) ze[j] = at[32 + l16];
-                else if constexpr (PER == 2) ze[j] = *reinterpret_cast<const uint16_t*>(at + 64 + l16 * 2);
-                else ze[j] = *reinterpret_cast<const uint32_t*>(at + 128 + l16 * 4);
-                continue;
+                const uint8_t* const at = lds + slot + S_AT + (wn * JB + j) * (64 * PER) + 32 * PER + l16 * PER;
+                if constexpr (PER == 1) sz[j] = *at;
+                else if constexpr (PER == 2) sz[j] = *reinterpret_cast<const uint16_t*>(at);
+                else sz[j] = *reinterpret_cast<const uint32_t*>(at);
+            } else if constexpr (FOLD) {
+                sz[j] = zen[j] & zero_mask;
+            } else {
+                sz[j] = scn[j] | (zen[j] & zero_mask) << 16;
             }
-            if constexpr (FOLD) ze[j] = zen[j] & zero_mask;
-            else sc[j][0] = scn[j][0] | (zen[j] & zero_mask) << 16;
         }
     };
     // FOLD, at the start of a stage: its scales, and what the sums of the last group still need
@@ -252,6 +244,7 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
     const int row_at = (wm * IB * 16 + l16) * 256, w_at = X_BYTES + wn * JB * kTileBytes + lane * 16;
     uint32_t cur = 0, nxt = STAGE, prv = (NST - 1) * STAGE;   // the ring's bytes of this, the next and the last stage
     // (not FOLD: from one address, the swizzle's by an exclusive or, so that there are not four of them to keep)
+    static_assert(STAGE % 256 == 0, "the k-step is in the address's bits 6 and 7");
     const uint32_t row_of = gemm_dev::lds_addr(lds) + row_at + ((g ^ l16) << 4);
     auto row_block = [&](int i, int ks) {                // k-steps from 4 on are the next stage's
         if constexpr (!FOLD) {
@@ -267,7 +260,7 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
     float one = 1.0f;
     asm volatile("" : "+s"(mask), "+v"(bits), "+s"(one));
     typename CodesOf<TY>::type s[JB];
-    auto zero_of = [&](int j, int p) { return 8 + (int)(int8_t)(FOLD ? ze[j] >> (8 * p) : sc[j][0] >> 16); };
+    auto zero_of = [&](int j, int p) { return 8 + (int)(int8_t)(sz[j] >> (FOLD ? 8 * p : 16)); };
     // READY: before this unit of work a barrier says that the next stage is there, before the last one of all, FREE, another that
     // this stage is read and may be filled; the copies follow in the gaps of three units.  The wait at READY leaves the copies of
     // the NST - 2 stages behind the next one under way, and counts on the last of these being issued by then.
@@ -318,15 +311,15 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
 #pragma unroll
         for (int r = 0; r < 4; ++r) out[r] = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(16 * g + 4 * r, __builtin_bit_cast(int, v)));
     };
-    auto begin_group = [&](int j, int p, float (&by)[4]) {
-        const float scale = (float)__builtin_bit_cast(_Float16, (uint16_t)(sc[j][p / 2] >> (16 * (p & 1))));
+    auto begin_group = [&](int j, float (&by)[4]) {      // (a stage is a group)
+        const float scale = (float)__builtin_bit_cast(_Float16, (uint16_t)sz[j]);
         off[j] = scale == 0.0f;
         const float to = off[j] ? unit_of[j] : scale, inverse = __builtin_amdgcn_rcpf(to);
         float ratio = unit_of[j] * inverse;              // one step on the division's remainder: 1 for equal scales
         ratio = __builtin_fmaf(__builtin_fmaf(-to, ratio, unit_of[j]), inverse, ratio);
         to_outputs(ratio, by);
         unit_of[j] = to;
-        s[j].set(off[j] ? 0 : zero_of(j, p));
+        s[j].set(off[j] ? 0 : zero_of(j, 0));
     };
     auto pair = [&](int kt, int v) __attribute__((always_inline)) {
         const int ks = v / PAIRS, next = (v + 1) % UNITS, nks = next / PAIRS, nj = next % PAIRS * 2;
@@ -335,7 +328,7 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int j = v % PAIRS * 2 + h, gap = i * 2 + h, block = gap / IB, piece = gap % IB;
-                if (ks % (4 / PER) == 0) {
+                if (ks == 0) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[i][j][r] *= change[v & 1][h][r];
                 }
@@ -343,7 +336,7 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
                 copies_of(kt, v, gap);
                 if (v == 2 && gap % (GAPS / JB) == 0) fetch(kt + 1, gap / (GAPS / JB));
                 if (piece == 0) {
-                    if (nks % (4 / PER) == 0) begin_group(nj + block, nks * PER / 4, change[next & 1][block]);
+                    if (nks == 0) begin_group(nj + block, change[next & 1][block]);
                     if (off[nj + block]) w[block] = 0;
                 }
                 s[nj + block].widen(piece, w[block], b[next & 1][block], mask, bits, one);
@@ -383,7 +376,7 @@ __global__ __launch_bounds__(OCC == 2 ? 512 : WM * WN * KS * 64, OCC) void w4g_t
             if constexpr (FOLD) {
                 s[j].set(zero_of(j, 0));
             } else {
-                begin_group(j, 0, change[0][j]);
+                begin_group(j, change[0][j]);
                 if (off[j]) w[j] = 0;
             }
 #pragma unroll
