@@ -216,22 +216,32 @@ __device__ __forceinline__ bool route_token(const MoeRouteArgs& a, int t, const 
     F sum = 0, mine = 0, last = INFINITY;                // mine, id: of slot `lane`
     float last_l = 0.0f, last_b = 0.0f;
     int id = -1;
-    for (int j = 0; j <= a.top_k; ++j) {
+    for (int j = 0; j < a.top_k; ++j) {
         int e = -1;
         F s = 0;
         float l = 0.0f, b = 0.0f;
         const F v = pick(e, s, l, b);
         if (v == kOut) break;
-        // a score that fp32 still holds all bits of, and weights are made of (in a sum of smaller ones they would vanish)
-        if (!EXACT && j < a.top_k) sure = sure && s >= (F)0x1p-100;
-        // equal for certain (the index decides), or apart for certain
-        if (j > 0) sure = sure && ((l == last_l && b == last_b) || last - v > apart + rounding * fabs(last));
-        if ((!EXACT && !sure) || j == a.top_k) break;
+        if constexpr (!EXACT) {
+            // a score that fp32 still holds all bits of, and weights are made of (in a sum of smaller ones they would vanish)
+            sure = sure && s >= (F)0x1p-100;
+            // equal for certain (the index decides), or apart for certain
+            if (j > 0) sure = sure && ((l == last_l && b == last_b) || last - v > apart + rounding * fabs(last));
+            if (!sure) break;
+        }
         last = v;
         last_l = l;
         last_b = b;
         sum += s;
         if (lane == j) { mine = s; id = e; }
+    }
+    // the same of all that are left against the last one chosen: behind one that is equal to it another may be larger
+    if (!EXACT && sure) {
+        bool near = false;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i)
+            near = near || (choice[i] > kOut && !(logit[i] == last_l && bias[i] == last_b) && !(last - choice[i] > apart + rounding * fabs(last)));
+        sure = __ballot(near) == 0;
     }
     if (!EXACT && !sure) return false;
     if (lane < a.top_k) {
