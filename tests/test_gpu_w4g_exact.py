@@ -134,3 +134,44 @@ def test_a_scale_that_is_no_number_spoils_its_own_channel_only(forced, form, bad
     forced(form)
     keep = [n for n in range(N) if n not in (17, 200)]
     _once_rounded(api.quik_linear_w4g(x, w)[:, keep], value[:, None] * W.T[at][:, keep], "float16")
+
+
+@pytest.mark.parametrize("form", range(13))
+@pytest.mark.parametrize("d", [1.0, 2.0 ** 12])
+def test_the_largest_bf16_activations(forced, form, d):
+    """Up to 2^104 / d, d the largest quotient of two scales of a channel: no sum leaves fp32.  Tolerance as above."""
+    import torch
+    from paper_2310_09259_amd import api
+    T, K, N = 260, 4096, 40
+    rng = np.random.Generator(np.random.PCG64(form))
+    w_q, s, z, _, _ = layer(form, N, K, 128, True)
+    s = np.where(rng.random(s.shape) < 0.5, 1.0, d).astype(np.float16) * np.float16(2.0 ** -12)
+    q = ((w_q[..., :K // 2, None] >> np.array([0, 4])) & 15).reshape(N, K).astype(np.int64)
+    of = np.arange(K) // 128
+    q = q - 16 * (q > 7) - z.astype(np.int64)[:, of]
+    W = q * s.astype(np.float64)[:, of]
+    w = pack((w_q, s, z), K, 128)
+    x = activations(form, T, K, "bfloat16").clamp(-1, 1) * (2.0 ** 103 / d)
+    forced(form)
+    y = api.quik_linear_w4g(x, w).double().cpu().numpy()
+    xs = x.double().cpu().numpy()
+    ref = xs @ W.T
+    tol = 2.0 ** -24 * (K + 8 + 4 * 32) * (np.abs(xs) @ (np.abs(s.astype(np.float64))[:, of] * (np.abs(q) + 136.0)).T)
+    assert np.isfinite(y).all() and np.all(np.abs(y - ref) <= STEP["bfloat16"] * (np.abs(ref) + tol) + tol)
+
+
+@pytest.mark.parametrize("form", range(13))
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+def test_rows_that_are_no_numbers_spoil_no_other_row(forced, form, dtype):
+    import torch
+    from paper_2310_09259_amd import api
+    T, K, N = 300, 392, 272
+    w = pack(layer(form, N, K, 128, True), K, 128)
+    x = activations(3, T, K, dtype)
+    forced(form)
+    clean = api.quik_linear_w4g(x, w)
+    keep = torch.ones(T, dtype=torch.bool, device="cuda")
+    for t, v in ((0, float("nan")), (17, float("inf")), (140, -float("inf")), (299, float("nan"))):
+        x[t, t % 128::5] = v
+        keep[t] = False
+    assert torch.equal(api.quik_linear_w4g(x, w)[keep], clean[keep])
