@@ -86,3 +86,28 @@ def test_a_stage_is_read_only_behind_a_wait_for_its_copies(tmp_path):
         if late:
             bad[form] = sorted(late)
     assert not bad, bad
+
+
+def test_waves_that_split_k_wait_for_their_own_tile(tmp_path):
+    """The kernels with private rings: a turn of the loop waits for its LDS reads, fills the stage they came from, leaves exactly
+    the later stages' copies under way, and reads."""
+    if not os.path.exists(OBJDUMP):
+        pytest.skip("no llvm-objdump")
+    forms = 0
+    for name, code in _kernels(str(tmp_path)).items():
+        m = re.search(r"w4g_rows_kernelINS_3w4g4(?:Half|Bf16)E((?:L[ib]\d+E)+)E", name)
+        if not m:
+            continue
+        forms += 1
+        _, blocks_m, blocks_n, _, stages, _ = map(int, re.findall(r"L[ib](\d+)E", m[1]))
+        first, last = _k_loop(code)
+        body = code[first:last + 1]
+        copies = [i for i, ins in enumerate(body) if _is_copy(ins)]
+        reads = [i for i, ins in enumerate(body) if ins[1].startswith("ds_read")]
+        waits = {i: re.search(r"vmcnt\((\d+)\)", ins[2]) for i, ins in enumerate(body) if ins[1] == "s_waitcnt"}
+        vm = {i: int(w[1]) for i, w in waits.items() if w}
+        assert len(copies) == 4 * blocks_m + 2 * blocks_n, name
+        assert not any(ins[1].startswith(("global_load", "flat_load", "scratch_")) for ins in body), name
+        assert any(i < copies[0] and "lgkmcnt(0)" in body[i][2] for i in waits), name
+        assert min(reads) > max(copies) and any(max(copies) < i < min(reads) and n <= (stages - 1) * len(copies) for i, n in vm.items()), name
+    assert forms >= 60
