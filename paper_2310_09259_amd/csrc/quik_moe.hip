@@ -17,9 +17,9 @@ using namespace w4g;
 //
 // What bounds it: the chain of reductions over the wave, some ten of them one behind the other, and for one token the
 // latency of its logits; the bytes are nothing.  So maxima and sums go through the lanes' data paths (six vector
-// instructions, no trip to LDS), and scores are computed in fp32.  Choices are told apart as float64 tells them: a token whose
-// chosen ones, the first not chosen, or groups next to the border lie within the error of the fp32 scores of each other, or
-// one of whose chosen scores is below 2^-100, goes through the same in float64.  Four groups of experts are reduced side by
+// instructions, no trip to LDS), and scores are computed in fp32.  Choices are told apart as float64 tells them: a token two
+// of whose chosen ones, or any one left and the last one chosen, or groups next to the border lie within the error of the fp32
+// scores of each other, or one of whose chosen scores is below 2^-100, goes through the same in float64.  Four groups of experts are reduced side by
 // side.  4096 tokens and 256 experts in eight groups: 33 us all in float64, with shuffles through LDS; 24.9 one group after
 // another; 20 to 24 as it is, by the tokens that go through float64 (for one token 10.4 and 9.5).  These are for logits of a
 // standard deviation of 1.5; the bound is one of the largest score, and scores near 0 or 1 lie close together: over 256 experts
